@@ -364,6 +364,103 @@ int sfi_mixed_step_desc(sfi_ctx* ctx, const void* q, const void* K, const void* 
 int sfi_advance(sfi_ctx* ctx, int32_t* ctx_len, int32_t* recent_start, void* stream);
 
 /*
+ * ---- What stands around the step in a decode loop: rows written, read for a batch that shares them, weighed, dropped ----
+ *
+ * Rotary positions.  With f_i the angle that pair i (0 <= i < rot_dim / 2) turns per position, a row at position p has
+ *   (a, b) -> magnitude * (a cos(p f_i) - b sin(p f_i), b cos(p f_i) + a sin(p f_i))
+ * for the pairs (a, b) = elements (i, i + rot_dim / 2) of the head, or (2 i, 2 i + 1) with interleaved = 1; elements from rot_dim
+ * on are copied.  With w_i = base^(-2 i / rot_dim):
+ *   SFI_ROPE_PLAIN   f_i = w_i, or freqs[i] where freqs is given (any other rule)
+ *   SFI_ROPE_LINEAR  f_i = w_i / factor (positions interpolated)
+ *   SFI_ROPE_TURNS   f_i = w_i * (s + (1 - s) / factor), s = clip((orig_ctx w_i / 2 pi - low) / (high - low), 0, 1): pairs that turn
+ *                    more than `high` times in the context the model was trained on are left, below `low` times interpolated
+ *   SFI_ROPE_DIMS    the same with s = 1 - clip((i - lo) / (hi - lo), 0, 1), a ramp along the pairs' numbers: lo = floor(i(high)) >= 0,
+ *                    hi = ceil(i(low)) <= rot_dim - 1, i(n) = rot_dim ln(orig_ctx / (2 pi n)) / (2 ln base) (hi - lo at least 0.001)
+ * rot_dim: a multiple of 16 up to 128.  The angle is exact to 1e-15 of a turn times the position: positions in the millions lose nothing.
+ */
+enum { SFI_ROPE_PLAIN = 0, SFI_ROPE_LINEAR = 1, SFI_ROPE_TURNS = 2, SFI_ROPE_DIMS = 3 };
+typedef struct sfi_rope {
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t scaling;      /* SFI_ROPE_* */
+  int32_t orig_ctx;     /* TURNS, DIMS: rows of the context the model was trained on */
+  double base;          /* > 1 */
+  double factor;        /* LINEAR, TURNS, DIMS: > 0 */
+  double low, high;     /* TURNS, DIMS: turns, 0 < low < high */
+  double magnitude;     /* factor on sine and cosine; 0 selects 1 */
+  const double* freqs;  /* HOST [rot_dim / 2], read during the call, or NULL */
+} sfi_rope;
+/* The f_i of a rule -> freqs (HOST, [rot_dim / 2]).  Pure host arithmetic. */
+int sfi_rope_freqs(const sfi_rope* rope, double* freqs);
+/* The rule of this context's sfi_rope_append calls: a small table in the workspace, written by a kernel on `stream` (appends on other streams
+ * must be ordered behind it).  Once per context, or whenever the rule changes; `rope` is read during the call only. */
+int sfi_set_rope(sfi_ctx* ctx, const sfi_rope* rope, void* stream);
+
+/*
+ * New rows of every sequence: queries and keys rotated, keys and values written into the cache.  Sequence b gets n_new[b] <= max_new rows
+ * (n_new NULL: max_new), one in a decoding step, many behind a prompt; ctx_len[b] already counts them (as everywhere: the current
+ * token's row included), so new row t becomes cache row ctx_len[b] - n_new[b] + t.  Its position is pos[b] + t, or with pos NULL
+ * the number of its cache row (the two part where rows have been evicted).
+ *   q        bf16, head g of new row t of sequence b at q + b * q_stride_b + t * q_stride_t + g * 128 (strides in elements, multiples of 8: the
+ *            three may be parts of one projection's output); k, v the same with n_kv_heads heads.  q may be NULL (with q_out).
+ *   q_out    bf16 [B, max_new, Hq, 128] contiguous; may be q itself where that is laid out alike, and may not overlap q otherwise.
+ *   K, V     the cache as in the hot calls, written here.  n_new, pos: DEVICE int32 [B].
+ * Padding (t >= n_new[b]) is not read, and q_out keeps what it holds there.  A row whose block id is out of range is not written.
+ * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW).  Needs sfi_set_rope.
+ */
+int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* k, int64_t k_stride_b, int64_t k_stride_t,
+                    const void* v, int64_t v_stride_b, int64_t v_stride_t, const int32_t* ctx_len, const int32_t* n_new, const int32_t* pos,
+                    int32_t max_new, void* q_out, void* K, void* V, void* stream);
+
+/*
+ * sfi_dense_attn for a batch whose sequences hold the same first rows (a system prompt, a document), which are read once for all:
+ * out[b, g, :] = attention of q[b, g] over rows [0, shared_len[b]) of sequence `lead` followed by rows [shared_len[b], ctx_len[b]) of
+ * sequence b.  Where the first shared_len[b] rows of b are those of the lead, that is sfi_dense_attn; rows of b below shared_len[b]
+ * are not used, and need not hold anything (in a paged cache their table entries are not read: usually they name the lead's blocks).
+ * Sequences may share different lengths of the lead's rows, or none (0).
+ *   shared_len  DEVICE int32 [B], brought into [0, min(ctx_len[b], ctx_len[lead], max_shared)] (SFI_GUARD_SHARED); the lead's own entry may be
+ *               anything in that range.
+ *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
+ * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums.
+ */
+int sfi_shared_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* ctx_len, const int32_t* shared_len,
+                    int32_t lead, int32_t max_shared, int32_t max_len, void* out, void* stream);
+
+/*
+ * sfi_dense_attn that also keeps the running weight of every row, what an eviction ranks by: for t < ctx_len[b]
+ *   weights_out[b, h, t] = decay * weights[b, h, t] + (1 / G) sum_{g in group h} softmax over [0, ctx_len[b]) of the logits of head g, at t
+ * weights, weights_out: DEVICE fp32 [B, Hkv, max_ctx] contiguous (max_ctx of the context), the same array or two that do not overlap;
+ * weights NULL reads as zero.  decay in [0, 1] (1: plain sums).  Rows at or behind ctx_len[b] are not touched; they
+ * have to be zero when their row is appended (sfi_evict leaves them so).  Sink and recent rows are weighed like all others.
+ * Uses the logits buffer of the workspace: evidence left there by sfi_slow_attn is gone afterwards.
+ */
+int sfi_weight_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* ctx_len, int32_t max_len, float decay,
+                    const float* weights, float* weights_out, void* out, void* stream);
+
+/*
+ * Eviction: of every (sequence, KV head) keep the sink rows [0, n_sink), the min(budget, |J|) rows of J = [n_sink, ctx_len - recent) with
+ * the largest weights (equal weights: the lower row; a weight that is not above zero, NaN included, counts as zero) and the recent
+ * rows, in their order, as rows [0, ctx_len_out[b]) of another cache or of the same one:
+ *   ctx_len_out[b] = ctx_len[b] - |J| + min(budget, |J|);   recent_start_out[b] = max(n_sink, ctx_len_out[b] - recent)
+ *   kept[b, h, :]  = the rows of J that stay, ascending, entries behind n_kept[b, h] = min(budget, |J|) set to -1 (row stride `budget`)
+ *   weights_out, row_pos_out: the kept rows' entries of weights and row_pos moved alike; weights_out is zero from ctx_len_out[b] on.
+ * dst: the context of the cache that is written (strides, block table, max_ctx; the same batch and n_kv_heads; nothing else of it is used), which
+ * may be ctx itself.  K_out == K and V_out == V evicts in place: strides and page size have to be the same, and a block table of dst must name the
+ * same block at the same place or none of the sequence's.  Otherwise what is read and what is written may not overlap; rows of K_out, V_out behind
+ * ctx_len_out[b] are left as they are.
+ * weights, row_pos: [B, Hkv, max_ctx of ctx] contiguous, weights_out, row_pos_out: [B, Hkv, max_ctx of dst].  row_pos (int32, any per-row
+ * data, say each row's position) may be NULL, and so may row_pos_out, recent_start_out and weights_out, and kept with budget = 0;
+ * ctx_len_out may be ctx_len, weights_out weights and row_pos_out row_pos (with equal max_ctx).  max_len: upper bound of ctx_len[] (0 = max_ctx); min(max_len,
+ * n_sink + budget + recent) rows have to fit dst.  budget <= cfg.max_budget.
+ * Keys keep the positions they were rotated with: sfi_rope_append takes the next token's position in pos from then on, and index
+ * sets (sel_idx) and compact buffers are stale.  Rows that several sequences share (sfi_shared_attn over one set of blocks) can be evicted from in
+ * place only if they are sink rows, which never move.
+ */
+int sfi_evict(sfi_ctx* ctx, const void* K, const void* V, const int32_t* ctx_len, int32_t max_len, int32_t budget, const float* weights,
+              const int32_t* row_pos, const sfi_ctx* dst, void* K_out, void* V_out, int32_t* ctx_len_out, int32_t* recent_start_out,
+              float* weights_out, int32_t* row_pos_out, int32_t* kept, int32_t* n_kept, void* stream);
+
+/*
  * Per-kernel timing for benchmarks.  sfi_set_profiling(ctx, max_calls) with max_calls > 0 makes each
  * of the next max_calls hot calls bracket every kernel it launches with a pair of HIP events on the
  * caller's stream (no host synchronisation in between); max_calls = 0 switches it off.
@@ -382,7 +479,7 @@ enum {
   SFI_STAGE_WRITE = 5,    /* ordered index write; short J: the whole selection, with the scoring and the output's merge
                              where no SCORE stage ran in a slow step */
   SFI_STAGE_ATTN2 = 6,    /* the fast sequences' attention of a mixed step, where it is a launch of its own */
-  SFI_STAGE_REORG = 7,    /* compact-buffer gather */
+  SFI_STAGE_REORG = 7,    /* rows copied: compact-buffer gather, append of new rows, the kept rows of an eviction */
   SFI_N_STAGES = 8
 };
 int sfi_set_profiling(sfi_ctx* ctx, int max_calls);
@@ -465,6 +562,8 @@ int sfi_plan_splits(const sfi_ctx* ctx, int32_t max_len, int32_t sel_stride, int
 #define SFI_GUARD_N_SEL 2   /* an n_sel[b, h] was negative or above sel_stride */
 #define SFI_GUARD_SEL_IDX 4 /* an index among sel_idx[b, h, 0:n_sel] was outside [0, ctx_len[b]) */
 #define SFI_GUARD_BLOCK 8   /* a block-table entry covering rows [0, ctx_len[b]) was outside [0, n_blocks) */
+#define SFI_GUARD_N_NEW 16  /* an n_new[b] was negative or above max_new or ctx_len[b] */
+#define SFI_GUARD_SHARED 32 /* a shared_len[b] was negative or above max_shared, ctx_len[b] or ctx_len[lead] */
 int sfi_device_status(sfi_ctx* ctx, int32_t* flags, int32_t clear, void* stream);
 
 /*

@@ -40,13 +40,22 @@ class SfiConfig(C.Structure):
     ]
 
 
+class SfiRope(C.Structure):
+    _fields_ = [
+        ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("orig_ctx", C.c_int32),
+        ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double),
+        ("freqs", C.POINTER(C.c_double)),
+    ]
+
+
 _lib: Optional[C.CDLL] = None
 _hot = None  # the CPython module with the hot calls
 
 EXPORTS = ("sfi_workspace_bytes", "sfi_create", "sfi_set_block_table", "sfi_destroy", "sfi_strerror", "sfi_slow_step", "sfi_slow_attn",
            "sfi_slow_select", "sfi_evidence_add", "sfi_evidence_add_causal", "sfi_evidence_select", "sfi_dense_attn",
            "sfi_fast_step", "sfi_fast_step_static", "sfi_fast_step_floor", "sfi_dense_attn_floor", "sfi_reorg", "sfi_fast_step_compact", "sfi_mixed_step", "sfi_mixed_step_compact", "sfi_step_begin", "sfi_mixed_step_desc", "sfi_trigger", "sfi_advance", "sfi_set_profiling", "sfi_stage_times",
-           "sfi_set_tuning", "sfi_set_dense_k_layout", "sfi_set_mixed_plan", "sfi_set_handover", "sfi_set_dense_scores", "sfi_plan_splits", "sfi_device_status", "sfi_query_splits")
+           "sfi_set_tuning", "sfi_set_dense_k_layout", "sfi_set_mixed_plan", "sfi_set_handover", "sfi_set_dense_scores", "sfi_plan_splits", "sfi_device_status", "sfi_query_splits",
+           "sfi_rope_freqs", "sfi_set_rope", "sfi_rope_append", "sfi_shared_attn", "sfi_weight_attn", "sfi_evict")
 
 
 def load_library() -> C.CDLL:
@@ -126,6 +135,18 @@ def load_library() -> C.CDLL:
     lib.sfi_device_status.argtypes = [vp, C.POINTER(i32), i32, vp]
     lib.sfi_query_splits.restype = C.c_int
     lib.sfi_query_splits.argtypes = [vp, C.POINTER(i32), C.POINTER(i32)]
+    lib.sfi_rope_freqs.restype = C.c_int
+    lib.sfi_rope_freqs.argtypes = [C.POINTER(SfiRope), C.POINTER(C.c_double)]
+    lib.sfi_set_rope.restype = C.c_int
+    lib.sfi_set_rope.argtypes = [vp, C.POINTER(SfiRope), vp]
+    lib.sfi_rope_append.restype = C.c_int
+    lib.sfi_rope_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.sfi_shared_attn.restype = C.c_int
+    lib.sfi_shared_attn.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]
+    lib.sfi_weight_attn.restype = C.c_int
+    lib.sfi_weight_attn.argtypes = [vp, vp, vp, vp, vp, i32, C.c_float, vp, vp, vp, vp]
+    lib.sfi_evict.restype = C.c_int
+    lib.sfi_evict.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -294,6 +315,67 @@ def sfi_advance(ctx, ctx_len, recent_start, stream=None) -> None:
     (_hot or _load_hot()).sfi_advance(ctx, ctx_len, recent_start, stream)
 
 
+ROPE_PLAIN, ROPE_LINEAR, ROPE_TURNS, ROPE_DIMS = 0, 1, 2, 3
+ROPE_SCALINGS = {"linear": ROPE_LINEAR, "turns": ROPE_TURNS, "dims": ROPE_DIMS}
+
+
+def _rope(rot_dim, base, interleaved, scaling, magnitude, freqs) -> SfiRope:
+    r = SfiRope()
+    r.rot_dim, r.interleaved, r.base, r.magnitude = rot_dim, int(interleaved), base, magnitude
+    if scaling is not None:
+        known = {"kind", "factor"} if scaling["kind"] == "linear" else {"kind", "factor", "low", "high", "orig_ctx"}
+        if set(scaling) != known:
+            raise ValueError(f"scaling of kind {scaling['kind']!r} takes {sorted(known)}, got {sorted(scaling)}")
+        r.scaling, r.factor = ROPE_SCALINGS[scaling["kind"]], scaling["factor"]
+        r.low, r.high, r.orig_ctx = scaling.get("low", 0.0), scaling.get("high", 0.0), scaling.get("orig_ctx", 0)
+    if freqs is not None:
+        if len(freqs) != rot_dim // 2:
+            raise ValueError(f"freqs holds {len(freqs)} values, {rot_dim // 2} are wanted")
+        r.freqs = (C.c_double * max(1, len(freqs)))(*freqs)
+    return r
+
+
+def sfi_rope_freqs(rot_dim: int, base: float, scaling: Optional[dict] = None):
+    """Angle per position of each pair (list of rot_dim / 2 floats).  scaling: None, or a dict with "kind" ("linear", "turns" or "dims")
+    and "factor", for the latter two "low", "high" and "orig_ctx" as well (include/sfi.h has the formulas)."""
+    f = (C.c_double * 64)()
+    _check(load_library().sfi_rope_freqs(C.byref(_rope(rot_dim, base, False, scaling, 0.0, None)), f), "sfi_rope_freqs")
+    return list(f[:rot_dim // 2])
+
+
+def sfi_set_rope(ctx, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: Optional[dict] = None,
+                 magnitude: float = 1.0, freqs=None, stream=None) -> None:
+    """The rotary rule of this context's sfi_rope_append calls; freqs: the angles per position themselves, in place of base and scaling."""
+    r = _rope(rot_dim, base, interleaved, scaling, magnitude, freqs)
+    _check(load_library().sfi_set_rope(ctx, C.byref(r), _stream(stream)), "sfi_set_rope")
+
+
+def sfi_rope_append(ctx, q, k, v, ctx_len, n_new, pos, q_out, K, V, stream=None) -> None:
+    """q: bf16 tensor [B, new, Hq, 128], k, v: [B, new, Hkv, 128], the heads of a row contiguous (views of one projection's output will do);
+    q and q_out (contiguous) may be None together.  n_new, pos: int32 [B] or None."""
+    for t in (q, k, v):
+        assert t is None or (t.dim() == 4 and t.shape[1] == k.shape[1] and t.stride(3) == 1 and (t.shape[2] == 1 or t.stride(2) == t.shape[3]))
+    assert q_out is None or q_out.is_contiguous()
+    (_hot or _load_hot()).sfi_rope_append(ctx, q, 0 if q is None else q.stride(0), 0 if q is None else q.stride(1), k, k.stride(0), k.stride(1),
+                                          v, v.stride(0), v.stride(1), ctx_len, n_new, pos, k.shape[1], q_out, K, V, stream)
+
+
+def sfi_shared_attn(ctx, q, K, V, ctx_len, shared_len, lead: int, max_shared: int, max_len: int, out, stream=None) -> None:
+    (_hot or _load_hot()).sfi_shared_attn(ctx, q, K, V, ctx_len, shared_len, lead, max_shared, max_len, out, stream)
+
+
+def sfi_weight_attn(ctx, q, K, V, ctx_len, max_len: int, decay: float, weights, weights_out, out, stream=None) -> None:
+    """weights (None: zero) and weights_out: fp32 [B, Hkv, max_ctx] contiguous, possibly the same tensor."""
+    (_hot or _load_hot()).sfi_weight_attn(ctx, q, K, V, ctx_len, max_len, decay, weights, weights_out, out, stream)
+
+
+def sfi_evict(ctx, K, V, ctx_len, max_len: int, budget: int, weights, row_pos, dst, K_out, V_out, ctx_len_out, recent_start_out, weights_out,
+              row_pos_out, kept, n_kept, stream=None) -> None:
+    """dst: handle of the context of the cache K_out, V_out (ctx itself to evict in place)."""
+    (_hot or _load_hot()).sfi_evict(ctx, K, V, ctx_len, max_len, budget, weights, row_pos, dst, K_out, V_out, ctx_len_out, recent_start_out,
+                                    weights_out, row_pos_out, kept, n_kept, stream)
+
+
 def sfi_set_profiling(ctx, max_calls: int) -> None:
     _check(load_library().sfi_set_profiling(ctx, int(max_calls)), "sfi_set_profiling")
 
@@ -332,7 +414,7 @@ def sfi_plan_splits(ctx, max_len: int, sel_stride: int) -> Tuple[int, int]:
     return d.value, f.value
 
 
-GUARD_CTX_LEN, GUARD_N_SEL, GUARD_SEL_IDX, GUARD_BLOCK = 1, 2, 4, 8
+GUARD_CTX_LEN, GUARD_N_SEL, GUARD_SEL_IDX, GUARD_BLOCK, GUARD_N_NEW, GUARD_SHARED = 1, 2, 4, 8, 16, 32
 
 
 def sfi_device_status(ctx, clear: bool = True, stream=None) -> int:

@@ -25,6 +25,8 @@ struct sfi_ctx {
   int mixed_plan;           // the ragged step's dense launch plans itself on the device (default; A/B knob, sfi_set_mixed_plan)
   int handover;             // fast-step records: 0 device scope, 1 XCD-local where the launch allows it (default), 2 (sfi_set_handover)
   int dense_scores;         // the slow step's dense launch scores: 0 no, 1 where that is faster (default), others for tests (sfi_set_dense_scores)
+  int rope_dim, rope_interleaved;  // rotary positions (sfi_set_rope); rope_dim 0: not set
+  float rope_magnitude;
   int last_dense_splits, last_fast_splits;
   int last_dense_scored;    // the last dense launch of a slow step has scored
   int met_dirty;            // 1: a step that scored there ended with an error: its statistics may still be in ws.met; 2: and the step
@@ -124,6 +126,8 @@ size_t carve(const sfi_config* c, char* base, Workspace* ws) {
   ws->segstat = full ? (double*)take((size_t)(B * Hkv) * n_seg * kSegStats * sizeof(double)) : nullptr;
   ws->slow_list = (int32_t*)take((4 + 4 * (size_t)B) * sizeof(int32_t));
   ws->seq_rec = (int32_t*)take((size_t)B * sizeof(int32_t));
+  ws->rope = (uint64_t*)take(kHeadDim / 2 * sizeof(uint64_t));
+  ws->moved = (uint32_t*)take((1 + (size_t)(B * Hkv) * (ld / kMoveRows)) * sizeof(uint32_t));
   ws->ld_pos = ld;
   ws->n_seg_cap = n_seg;
   return off;
@@ -729,7 +733,8 @@ namespace {
 // First half of a slow step: dense attention with the evidence (y over J, Selector state cleared,
 // J-only softmax statistics) left in the workspace.
 int slow_attn_impl(sfi_ctx* x, const void* q, const void* K, const void* V, const int32_t* ctx_len, int ml,
-                   float* out, hipStream_t st, bool merge_later = false, const int32_t* q_len = nullptr, bool select_next = false) {
+                   float* out, hipStream_t st, bool merge_later = false, const int32_t* q_len = nullptr, bool select_next = false,
+                   bool rounded = false) {
   AttnArgs a;
   fill_attn(x, &a, q, K, V, ctx_len);
   a.q_len = q_len;
@@ -751,7 +756,7 @@ int slow_attn_impl(sfi_ctx* x, const void* q, const void* K, const void* V, cons
   x->last_dense_scored = select_next && score_in_dense(x, a, ml);
   if (x->last_dense_scored && set_dense_scores(x, &a, st) != SFI_OK) return SFI_ELAUNCH;
   x->last_dense_splits = a.n_split;
-  { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_attn_dense(a, x->cfg.batch, a.n_split, st)); if (!t.stop()) return SFI_ELAUNCH; }
+  { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_attn_dense(a, x->cfg.batch, a.n_split, st, rounded)); if (!t.stop()) return SFI_ELAUNCH; }
   if (merge_later) return SFI_OK;  // the Selector's scoring launch merges
   MergeArgs m{x->ws.part, out, nullptr, x->cfg.n_q_heads, a.n_split, 0, 0, x->ws.jstat, a.plan_batch > 0 ? x->ws.seq_rec : nullptr, x->G, x->alpha, x->cfg.out_bf16};
   { StageTimer t(x, st, SFI_STAGE_MERGE); SFI_TRY(launch_merge(m, x->cfg.batch, st)); if (!t.stop()) return SFI_ELAUNCH; }
@@ -1375,6 +1380,252 @@ int sfi_query_splits(const sfi_ctx* x, int32_t* dense_splits, int32_t* fast_spli
   if (dense_splits) *dense_splits = x->last_dense_splits;
   if (fast_splits) *fast_splits = x->last_fast_splits;
   return SFI_OK;
+}
+
+// ---- rotary positions, attention over shared rows and with running weights, eviction -------------------------------------------
+namespace {
+// What pair i turns per position, in radians (include/sfi.h has the formulas).
+int rope_freqs(const sfi_rope* r, double* f) {
+  if (r == nullptr || f == nullptr) return SFI_EINVAL;
+  if (r->rot_dim < 2 || r->rot_dim > kHeadDim) return SFI_EINVAL;
+  if (r->rot_dim % 16 != 0) return SFI_EUNSUPPORTED;
+  if (r->interleaved != 0 && r->interleaved != 1) return SFI_EINVAL;
+  if (!(r->magnitude >= 0.0) || !(r->magnitude <= 1e6)) return SFI_EINVAL;
+  const int n = r->rot_dim, half = n / 2;
+  if (r->freqs != nullptr) {
+    if (r->scaling != SFI_ROPE_PLAIN) return SFI_EINVAL;
+    for (int i = 0; i < half; ++i) {
+      if (!(fabs(r->freqs[i]) <= 1e9)) return SFI_EINVAL;
+      f[i] = r->freqs[i];
+    }
+    return SFI_OK;
+  }
+  if (!(r->base > 1.0) || !(r->base <= 1e30)) return SFI_EINVAL;
+  if (r->scaling != SFI_ROPE_PLAIN && (!(r->factor > 0.0) || !(r->factor <= 1e9))) return SFI_EINVAL;
+  if (r->scaling == SFI_ROPE_TURNS || r->scaling == SFI_ROPE_DIMS) {
+    if (r->orig_ctx < 1 || !(r->low > 0.0) || !(r->high > r->low) || !(r->high <= 1e30)) return SFI_EINVAL;
+  } else if (r->scaling != SFI_ROPE_PLAIN && r->scaling != SFI_ROPE_LINEAR) {
+    return SFI_EUNSUPPORTED;
+  }
+  const double two_pi = 6.283185307179586476925;
+  for (int i = 0; i < half; ++i) {
+    f[i] = pow(r->base, -2.0 * i / n);
+    double keep = 1.0;
+    if (r->scaling == SFI_ROPE_LINEAR) {
+      keep = 0.0;
+    } else if (r->scaling == SFI_ROPE_TURNS) {
+      keep = (r->orig_ctx * f[i] / two_pi - r->low) / (r->high - r->low);
+    } else if (r->scaling == SFI_ROPE_DIMS) {
+      const double per = n / (2.0 * log(r->base));
+      const double lo = fmax(floor(per * log(r->orig_ctx / (two_pi * r->high))), 0.0);
+      const double hi = fmin(ceil(per * log(r->orig_ctx / (two_pi * r->low))), n - 1.0);
+      keep = 1.0 - (i - lo) / fmax(hi - lo, 0.001);
+    }
+    keep = fmin(fmax(keep, 0.0), 1.0);
+    if (keep < 1.0) f[i] = f[i] * (keep + (1.0 - keep) / r->factor);
+  }
+  return SFI_OK;
+}
+// The context as the operators below use it: every row ranks (no sink or recent rows apart), by the mean weight alone.
+void all_rows_view(const sfi_ctx* x, sfi_ctx* y) {
+  *y = *x;
+  y->cfg.n_sink = y->cfg.recent = 0;
+  y->cfg.selector_mode = 0;
+  y->alpha = 1.0f;
+}
+// Splits of the shared rows (none where nothing can be shared) and of each sequence's own.
+void shared_splits(const sfi_ctx* x, SharedArgs* a) {
+  const int cols = shared_cols(a->B * a->G), groups = (a->B * a->G + cols - 1) / cols;
+  auto splits = [&](int tiles, int64_t cells, int cap) {
+    int64_t s = x->n_cu / cells;
+    s = std::min<int64_t>(s, (tiles + kWaves - 1) / kWaves);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, cap));
+  };
+  a->n_shared = a->max_shared > 0 ? splits((a->max_shared + kTile - 1) / kTile, (int64_t)a->Hkv * groups, 40) : 0;
+  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 20);
+}
+}  // namespace
+
+int sfi_rope_freqs(const sfi_rope* rope, double* freqs) { return rope_freqs(rope, freqs); }
+
+int sfi_set_rope(sfi_ctx* x, const sfi_rope* rope, void* stream) {
+  if (x == nullptr) return SFI_EINVAL;
+  double f[kHeadDim / 2];
+  const int rc = rope_freqs(rope, f);
+  if (rc != SFI_OK) return rc;
+  RopeTable t;
+  memset(&t, 0, sizeof(t));
+  for (int i = 0; i < rope->rot_dim / 2; ++i) {
+    long double turns = (long double)f[i] / 6.283185307179586476925286766559L;
+    turns = (turns - floorl(turns)) * 18446744073709551616.0L;
+    t.turn[i] = turns >= 18446744073709551615.0L ? 0u : (uint64_t)(turns + 0.5L);
+  }
+  SFI_TRY(launch_rope_table(t, x->ws.rope, (hipStream_t)stream));
+  x->rope_dim = rope->rot_dim;
+  x->rope_interleaved = rope->interleaved;
+  x->rope_magnitude = rope->magnitude > 0.0 ? (float)rope->magnitude : 1.0f;
+  return SFI_OK;
+}
+
+int sfi_rope_append(sfi_ctx* x, const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* k, int64_t k_stride_b, int64_t k_stride_t,
+                    const void* v, int64_t v_stride_b, int64_t v_stride_t, const int32_t* ctx_len, const int32_t* n_new, const int32_t* pos,
+                    int32_t max_new, void* q_out, void* K, void* V, void* stream) {
+  if (x == nullptr || k == nullptr || v == nullptr || ctx_len == nullptr || K == nullptr || V == nullptr) return SFI_EINVAL;
+  if ((q == nullptr) != (q_out == nullptr)) return SFI_EINVAL;
+  if (x->rope_dim == 0 || max_new < 1 || max_new > x->cfg.max_ctx) return SFI_EINVAL;
+  if (x->cfg.page_size != 0 && x->table == nullptr) return SFI_EINVAL;  // paged cache without a block table
+  const int64_t st[6] = {q != nullptr ? q_stride_b : 0, q != nullptr ? q_stride_t : 0, k_stride_b, k_stride_t, v_stride_b, v_stride_t};
+  for (int i = 0; i < 6; ++i) {
+    if (st[i] < 0) return SFI_EINVAL;
+    if (st[i] % 8 != 0) return SFI_EALIGN;
+  }
+  if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(K, 16) || misaligned(V, 16) ||
+      misaligned(ctx_len, 4) || misaligned(n_new, 4) || misaligned(pos, 4))
+    return SFI_EALIGN;
+  const sfi_config& c = x->cfg;
+  if ((int64_t)c.batch * max_new >= (int64_t)1 << 32) return SFI_EUNSUPPORTED;  // one workgroup per four tokens
+  CallRecord call_record(x);
+  RopeArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.q_in_b = st[0]; a.q_in_t = st[1]; a.k_in_b = st[2]; a.k_in_t = st[3]; a.v_in_b = st[4]; a.v_in_t = st[5];
+  a.ctx_len = ctx_len; a.n_new = n_new; a.pos = pos;
+  a.q_out = (uint16_t*)q_out; a.K = (uint16_t*)K; a.V = (uint16_t*)V;
+  a.k_sb = c.k_stride_b; a.k_sh = c.k_stride_h; a.k_st = c.k_stride_t;
+  a.v_sb = c.v_stride_b; a.v_sh = c.v_stride_h; a.v_st = c.v_stride_t;
+  a.table = x->ws.rope; a.magnitude = x->rope_magnitude; a.rot = x->rope_dim; a.interleaved = x->rope_interleaved;
+  a.B = c.batch; a.Hq = q != nullptr ? c.n_q_heads : 0; a.Hkv = c.n_kv_heads; a.max_new = max_new;
+  a.block_table = x->table; a.table_stride = x->table_stride; a.page_lg = x->page_lg; a.page_rpb = x->page_rpb;
+  a.len_cap = c.max_ctx; a.n_blocks = x->n_blocks;
+  a.guard = x->ws.guard;
+  StageTimer t(x, (hipStream_t)stream, SFI_STAGE_REORG);
+  SFI_TRY(launch_rope_append(a, x->n_cu, (hipStream_t)stream));
+  return t.stop() ? SFI_OK : SFI_ELAUNCH;
+}
+
+int sfi_shared_attn(sfi_ctx* x, const void* q, const void* K, const void* V, const int32_t* ctx_len, const int32_t* shared_len, int32_t lead,
+                    int32_t max_shared, int32_t max_len, void* out, void* stream) {
+  int rc = check_common(x, q, K, V, ctx_len, out);
+  if (rc != SFI_OK) return rc;
+  if (shared_len == nullptr) return SFI_EINVAL;
+  if (misaligned(shared_len, 4)) return SFI_EALIGN;
+  int ml;
+  if ((rc = resolve_max_len(x, max_len, &ml)) != SFI_OK) return rc;
+  const sfi_config& c = x->cfg;
+  if (lead < 0 || lead >= c.batch || max_shared < 0 || max_shared > ml) return SFI_EINVAL;
+  if ((int64_t)c.batch * x->G > INT32_MAX / 2) return SFI_EUNSUPPORTED;
+  hipStream_t st = (hipStream_t)stream;
+  CallRecord call_record(x);
+  SharedArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = (const uint16_t*)q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
+  a.k_sb = c.k_stride_b; a.k_sh = c.k_stride_h; a.k_st = c.k_stride_t; a.v_sb = c.v_stride_b; a.v_sh = c.v_stride_h; a.v_st = c.v_stride_t;
+  a.ctx_len = ctx_len; a.shared_len = shared_len; a.part = x->ws.part;
+  a.table = x->table; a.table_stride = x->table_stride; a.page_lg = x->page_lg; a.page_rpb = x->page_rpb; a.n_blocks = x->n_blocks;
+  a.B = c.batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = x->G; a.lead = lead; a.max_shared = max_shared; a.len_cap = ml;
+  a.scale_log2 = (float)((double)x->scale * 1.4426950408889634);
+  a.guard = x->ws.guard;
+  shared_splits(x, &a);
+  if (a.n_shared > 0) { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_shared_rows(a, st)); if (!t.stop()) return SFI_ELAUNCH; }
+  { StageTimer t(x, st, SFI_STAGE_ATTN2); SFI_TRY(launch_own_rows(a, st)); if (!t.stop()) return SFI_ELAUNCH; }
+  MergeArgs m{x->ws.part, (float*)out, nullptr, c.n_q_heads, a.n_shared + a.n_own, 0, 0, nullptr, nullptr, x->G, x->alpha, c.out_bf16};
+  { StageTimer t(x, st, SFI_STAGE_MERGE); SFI_TRY(launch_merge(m, c.batch, st)); if (!t.stop()) return SFI_ELAUNCH; }
+  return SFI_OK;
+}
+
+int sfi_weight_attn(sfi_ctx* x, const void* q, const void* K, const void* V, const int32_t* ctx_len, int32_t max_len, float decay,
+                    const float* weights, float* weights_out, void* out, void* stream) {
+  int rc = check_common(x, q, K, V, ctx_len, out);
+  if (rc != SFI_OK) return rc;
+  if (weights_out == nullptr || !(decay >= 0.f) || !(decay <= 1.f)) return SFI_EINVAL;
+  if (misaligned(weights, 4) || misaligned(weights_out, 4)) return SFI_EALIGN;
+  int ml;
+  if ((rc = resolve_max_len(x, max_len, &ml)) != SFI_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  CallRecord call_record(x);
+  sfi_ctx y;  // for this call only
+  all_rows_view(x, &y);
+  y.dense_wide = 0;
+  rc = slow_attn_impl(&y, q, K, V, ctx_len, ml, (float*)out, st, true, nullptr, false, true);
+  x->last_dense_splits = y.last_dense_splits;
+  x->last_dense_planned = y.last_dense_planned;
+  if (rc != SFI_OK) return rc;
+  SelArgs sa;
+  fill_sel(&y, &sa, ctx_len, ml, nullptr, 0, y.last_dense_splits, nullptr, nullptr);
+  sa.part = y.ws.part;
+  sa.merge_out = (float*)out;
+  if (y.last_dense_planned) sa.seq_rec = y.ws.seq_rec;
+  sa.weights = weights; sa.w_out = weights_out; sa.w_rows = x->cfg.max_ctx; sa.decay = decay;
+  StageTimer t(x, st, SFI_STAGE_SCORE);
+  SFI_TRY(launch_sel_weigh(sa, x->cfg.batch, ml, st));
+  return t.stop() ? SFI_OK : SFI_ELAUNCH;
+}
+
+int sfi_evict(sfi_ctx* x, const void* K, const void* V, const int32_t* ctx_len, int32_t max_len, int32_t budget, const float* weights,
+              const int32_t* row_pos, const sfi_ctx* dst, void* K_out, void* V_out, int32_t* ctx_len_out, int32_t* recent_start_out,
+              float* weights_out, int32_t* row_pos_out, int32_t* kept, int32_t* n_kept, void* stream) {
+  if (x == nullptr || dst == nullptr || K == nullptr || V == nullptr || ctx_len == nullptr || weights == nullptr || K_out == nullptr ||
+      V_out == nullptr || ctx_len_out == nullptr || n_kept == nullptr || (kept == nullptr && budget != 0) || (row_pos_out != nullptr && row_pos == nullptr))
+    return SFI_EINVAL;
+  if (misaligned(K, 16) || misaligned(V, 16) || misaligned(K_out, 16) || misaligned(V_out, 16) || misaligned(ctx_len, 4) || misaligned(weights, 4) ||
+      misaligned(row_pos, 4) || misaligned(ctx_len_out, 4) || misaligned(recent_start_out, 4) || misaligned(weights_out, 4) ||
+      misaligned(row_pos_out, 4) || misaligned(kept, 4) || misaligned(n_kept, 4))
+    return SFI_EALIGN;
+  const sfi_config &c = x->cfg, &d = dst->cfg;
+  if (budget < 0 || budget > c.max_budget || d.batch != c.batch || d.n_kv_heads != c.n_kv_heads) return SFI_EINVAL;
+  if ((c.page_size != 0 && x->table == nullptr) || (d.page_size != 0 && dst->table == nullptr)) return SFI_EINVAL;
+  int ml;
+  int rc = resolve_max_len(x, max_len, &ml);
+  if (rc != SFI_OK) return rc;
+  const int64_t most64 = (int64_t)c.n_sink + c.recent + budget;
+  const int most = (int)std::min<int64_t>(ml, most64);  // rows that can be left
+  if (most > d.max_ctx) return SFI_EINVAL;
+  const bool in_place = K_out == K || V_out == V;
+  if (in_place) {  // both, and rows laid out alike
+    if (K_out != K || V_out != V || c.page_size != d.page_size || c.k_stride_b != d.k_stride_b || c.k_stride_h != d.k_stride_h ||
+        c.k_stride_t != d.k_stride_t || c.v_stride_b != d.v_stride_b || c.v_stride_h != d.v_stride_h || c.v_stride_t != d.v_stride_t ||
+        x->page_rpb != dst->page_rpb)
+      return SFI_EINVAL;
+  }
+  if ((weights_out == weights || (row_pos_out != nullptr && row_pos_out == row_pos)) && c.max_ctx != d.max_ctx) return SFI_EINVAL;
+  hipStream_t st = (hipStream_t)stream;
+  CallRecord call_record(x);
+  const int B = c.batch, nJ = ml - c.recent - c.n_sink;
+  const int n_chunks = (most + kMoveRows - 1) / kMoveRows;
+  if (((int64_t)n_chunks + 1) * B * c.n_kv_heads > INT32_MAX) return SFI_EUNSUPPORTED;
+  SelArgs sa;
+  fill_sel(x, &sa, ctx_len, ml, nullptr, budget, 0, kept, n_kept);
+  sa.weights = weights; sa.w_rows = c.max_ctx;
+  sa.guard = x->ws.guard;
+  if (in_place) { sa.moved = x->ws.moved; sa.moved_words = 1 + B * c.n_kv_heads * n_chunks; }
+  if (nJ <= kPickMax) {
+    StageTimer t(x, st, SFI_STAGE_WRITE);
+    SFI_TRY(launch_sel_pick(sa, B, nJ, 3, st));
+    if (!t.stop()) return SFI_ELAUNCH;
+  } else {
+    { StageTimer t(x, st, SFI_STAGE_SCORE); SFI_TRY(launch_sel_weights(sa, B, nJ, st)); if (!t.stop()) return SFI_ELAUNCH; }
+    { StageTimer t(x, st, SFI_STAGE_CAND); SFI_TRY(launch_sel_cand(sa, B, nJ, st)); if (!t.stop()) return SFI_ELAUNCH; }
+    { StageTimer t(x, st, SFI_STAGE_WRITE); SFI_TRY(launch_sel_write(sa, B, nJ, st)); if (!t.stop()) return SFI_ELAUNCH; }
+  }
+  MoveArgs a;
+  memset(&a, 0, sizeof(a));
+  a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.K_out = (uint16_t*)K_out; a.V_out = (uint16_t*)V_out;
+  a.k_sb = c.k_stride_b; a.k_sh = c.k_stride_h; a.k_st = c.k_stride_t; a.v_sb = c.v_stride_b; a.v_sh = c.v_stride_h; a.v_st = c.v_stride_t;
+  a.ko_sb = d.k_stride_b; a.ko_sh = d.k_stride_h; a.ko_st = d.k_stride_t; a.vo_sb = d.v_stride_b; a.vo_sh = d.v_stride_h; a.vo_st = d.v_stride_t;
+  a.table = x->table; a.table_stride = x->table_stride; a.page_lg = x->page_lg; a.page_rpb = x->page_rpb; a.n_blocks = x->n_blocks;
+  a.table_out = dst->table; a.table_out_stride = dst->table_stride; a.page_out_lg = dst->page_lg; a.page_out_rpb = dst->page_rpb;
+  a.n_blocks_out = dst->n_blocks;
+  a.state = x->ws.state; a.kept = kept; a.n_kept = n_kept;
+  a.w_in = weights; a.w_out = weights_out; a.pos_in = row_pos; a.pos_out = row_pos_out;
+  a.len_out = ctx_len_out; a.recent_out = recent_start_out;
+  a.ticket = x->ws.moved; a.flags = x->ws.moved + 1; a.flag_stride = n_chunks;
+  a.same_rows = in_place && x->table == dst->table;
+  a.w_in_rows = c.max_ctx; a.w_out_rows = d.max_ctx;
+  a.B = B; a.Hkv = c.n_kv_heads; a.n_sink = c.n_sink; a.recent = c.recent; a.budget = budget; a.n_chunks = n_chunks;
+  a.guard = x->ws.guard;
+  StageTimer t(x, st, SFI_STAGE_REORG);
+  SFI_TRY(launch_move_rows(a, in_place, st));
+  return t.stop() ? SFI_OK : SFI_ELAUNCH;
 }
 
 }  // extern "C"

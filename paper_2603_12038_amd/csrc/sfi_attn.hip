@@ -417,6 +417,14 @@ __device__ __forceinline__ void mask_tail(Tile& T, float (&y)[8], int jg, int p0
 // which is rare after the first tiles) and the weights as two bf16 terms, hi + lo ~ 16 bits.
 // Masked rows carry y = kNeg; every tile handed in has at least one unmasked row, so each head's
 // maximum is finite and 2^(kNeg - max) is exactly 0.
+// ROUND: both terms to nearest even, not cut off: the weights' loss is below 2^-17 and has no direction (cut off, a sum over few
+// rows of like weight is 6e-6 too small).
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+__device__ __forceinline__ uint32_t round2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+template <bool ROUND = false>
 __device__ __forceinline__ void softmax_phase(const float (&y)[8], f32x4 (&acc)[8], float& m_run, float& l_run, int jg,
                                               bf16x8& a_hi, bf16x8& a_lo) {
   float mt = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
@@ -434,6 +442,20 @@ __device__ __forceinline__ void softmax_phase(const float (&y)[8], f32x4 (&acc)[
     m_run = m_new;
   }
   float pr[8], lo[8], ps = 0.f;
+  if (ROUND) {
+    uint32_t hi[4], rest[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = fast_exp2(y[2 * i] - m_run), p1 = fast_exp2(y[2 * i + 1] - m_run);
+      ps += p0 + p1;
+      hi[i] = round2(p0, p1);
+      rest[i] = round2(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
+    }
+    l_run += ps;
+    a_hi = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    a_lo = as_bf16x8(make_uint4(rest[0], rest[1], rest[2], rest[3]));
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     pr[i] = fast_exp2(y[i] - m_run);
@@ -778,7 +800,7 @@ struct ListWalk {
 // dense kernel
 // ------------------------------------------------------------------------------------------------
 // PAGED: K / V are block pools addressed through the sequence's block table.
-// EXPOSE 1: also write y over J for the Selector; 2: y and the squared key norms; 3, 4: y (and the norms) stay in LDS as far as they fit, for score_tail.
+// EXPOSE 1: also write y over J for the Selector; -1: the same, with softmax_phase's ROUND (sfi_weight_attn); 2: y and the squared key norms; 3, 4: y (and the norms) stay in LDS as far as they fit, for score_tail.
 // BIG: twice the logits stash per wave, which leaves room for one workgroup per compute unit only
 // (launches where every sequence is dense, and the planned launch, run one per unit anyway; the ragged
 // step's launch with a workgroup per cell keeps two, although that kernel spills 6 to 26 of its 256 registers: with one,
@@ -1020,7 +1042,7 @@ __device__ __forceinline__ void dense_body(const AttnArgs& a, const DenseShare& 
     const int N = inJ ? NJ : NS;
     if (p0 + kTile > N) mask_tail<WIDE>(T, y, jg, p0, N);
     bf16x8 a_hi, a_lo;
-    softmax_phase(y, acc, m_run, l_run, jg, a_hi, a_lo);
+    softmax_phase<EXPOSE == -1>(y, acc, m_run, l_run, jg, a_hi, a_lo);
     pv_phase(T, a_hi, a_lo, acc);
     if (!kRefill) return;
     if (PAGED) issue_v_rows<uint64_t>(T, R, pra, prb);
@@ -2679,7 +2701,7 @@ hipError_t launch_trigger(const int32_t* last_token, const uint32_t* bitmap, int
 }
 
 template <bool PAGED>
-static void launch_dense_t(const AttnArgs& a, dim3 grid, hipStream_t s) {
+static void launch_dense_t(const AttnArgs& a, dim3 grid, bool rounded, hipStream_t s) {
   if (a.plan_batch > 0) {
     const dim3 pgrid(a.Hkv, std::max(a.plan_wgs, a.plan_even * a.plan_batch));
     const uint32_t strides = (uint32_t)a.ms | (uint32_t)a.fs << 16;
@@ -2688,10 +2710,15 @@ static void launch_dense_t(const AttnArgs& a, dim3 grid, hipStream_t s) {
                      a.q_len, strides, a.plan_batch, a.plan_wgs, 1.0f / (float)a.plan_min, a.n_sink, a.recent, a.len_cap, a)
     if (a.logits == nullptr) SFI_PLANNED(0);
     else if (a.with_knorm && a.met != nullptr) SFI_PLANNED(4);
+    else if (rounded) SFI_PLANNED(-1);
     else if (a.with_knorm) SFI_PLANNED(2);
     else if (a.met != nullptr) SFI_PLANNED(3);
     else SFI_PLANNED(1);
 #undef SFI_PLANNED
+    return;
+  }
+  if (rounded) {
+    hipLaunchKernelGGL((attn_dense_kernel<-1, PAGED, true>), grid, dim3(kAttnThreads), 0, s, a);
     return;
   }
   if constexpr (!PAGED) {
@@ -2724,10 +2751,10 @@ static void launch_dense_t(const AttnArgs& a, dim3 grid, hipStream_t s) {
     hipLaunchKernelGGL((attn_dense_kernel<0, PAGED>), grid, dim3(kAttnThreads), 0, s, a);
   }
 }
-hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s) {
+hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool rounded) {
   const dim3 grid(a.Hkv, n_slots, B);
-  if (a.table != nullptr) launch_dense_t<true>(a, grid, s);
-  else launch_dense_t<false>(a, grid, s);
+  if (a.table != nullptr) launch_dense_t<true>(a, grid, rounded, s);
+  else launch_dense_t<false>(a, grid, rounded, s);
   return hipGetLastError();
 }
 hipError_t launch_attn_ragged(const AttnArgs& d, const AttnArgs& f, bool balanced, hipStream_t s) {

@@ -59,7 +59,7 @@ __device__ __forceinline__ void store_out4(float* out, int64_t elem, float4 v, b
 }
 
 // Per (sequence, KV head) Selector state words.
-enum SelState { ST_BIN1 = 0, ST_K1 = 1, ST_CAND = 2 };
+enum SelState { ST_BIN1 = 0, ST_K1 = 1, ST_CAND = 2, ST_LEN = 4 };  // ST_LEN: eviction, ctx_len (clamped) as the selecting launch read it
 
 // A window query under the causal mask (Eq. window_logits): the query sits at row q_len - 1 of a context that ends
 // at row L_end - 1, sees rows [0, q_len) only, and its evidence covers the part of the allowed set
@@ -106,6 +106,8 @@ struct Workspace {
   uint32_t* wg_hist;  // [B*Hkv][kSlotCap][kHistBins]  ... mode 0: key histogram of each workgroup
   double* wg_stat;    // [B*Hkv][kSlotCap][kSegStats]  ... full Selector: each workgroup's sums for lambda*
   int32_t* guard;     // [1]  SFI_GUARD_* bits of device-side inputs the kernels found out of range and clamped
+  uint64_t* rope;     // [kHeadDim / 2]  rotary positions: what each pair turns per position, in 2^-64 of a turn
+  uint32_t* moved;    // [1 + B*Hkv * (ld / kMoveRows)]  eviction in place: counter the chunks are dealt by, chunks whose rows are in registers
   int64_t ld_pos;     // multiple of kSelSeg
   int32_t n_seg_cap;
 };
@@ -113,7 +115,7 @@ struct Workspace {
 // Device-side inputs (lengths, counts, row indices, block ids) are clamped into the range the launch may
 // touch before they address memory; a kernel that had to clamp ORs the matching bit into Workspace::guard
 // once, on its way out.  The bit values are the public SFI_GUARD_* ones.
-constexpr int kGuardCtxLen = 1, kGuardNSel = 2, kGuardSelIdx = 4, kGuardBlock = 8;
+constexpr int kGuardCtxLen = 1, kGuardNSel = 2, kGuardSelIdx = 4, kGuardBlock = 8, kGuardNNew = 16, kGuardShared = 32;
 
 struct AttnArgs {
   const uint16_t* q;
@@ -205,6 +207,79 @@ struct ReorgArgs {
 };
 constexpr int kReorgRows = 64;   // compact rows per workgroup of the Reorg kernel
 
+// Rotary positions and the append of new rows.
+struct RopeTable {
+  uint64_t turn[kHeadDim / 2];
+};
+struct RopeArgs {
+  const uint16_t *q, *k, *v;       // new rows: [B][max_new] tokens, heads of a token back to back
+  int64_t q_in_b, q_in_t, k_in_b, k_in_t, v_in_b, v_in_t;  // strides in elements
+  const int32_t* ctx_len;
+  const int32_t* n_new;            // nullptr: max_new rows for every sequence
+  const int32_t* pos;              // nullptr: a row's position is its cache row; else the position of each sequence's first new row
+  uint16_t* q_out;                 // [B][max_new][Hq][128]
+  uint16_t* K;
+  uint16_t* V;
+  int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  const uint64_t* table;           // Workspace::rope
+  float magnitude;
+  int32_t rot, interleaved;
+  int32_t B, Hq, Hkv, max_new;
+  const int32_t* block_table;      // paged cache (see AttnArgs)
+  int64_t table_stride;
+  int32_t page_lg, page_rpb;
+  int32_t len_cap, n_blocks;
+  int32_t* guard;
+};
+
+// Eviction: the kept rows to the front of another cache, or of the same one.
+constexpr int kMoveRows = 64;    // rows per workgroup
+struct MoveArgs {
+  const uint16_t* K;
+  const uint16_t* V;
+  int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  uint16_t* K_out;
+  uint16_t* V_out;
+  int64_t ko_sb, ko_sh, ko_st, vo_sb, vo_sh, vo_st;
+  const int32_t* table;            // paged caches (see AttnArgs)
+  const int32_t* table_out;
+  int64_t table_stride, table_out_stride;
+  int32_t page_lg, page_rpb, n_blocks, page_out_lg, page_out_rpb, n_blocks_out;
+  const uint32_t* state;           // Workspace::state
+  const int32_t* kept;             // [B*Hkv][budget]
+  const int32_t* n_kept;           // [B*Hkv]
+  const float* w_in;               // [B*Hkv][w_in_rows]
+  float* w_out;                    // [B*Hkv][w_out_rows] or nullptr
+  const int32_t* pos_in;           // as w_in, or nullptr
+  int32_t* pos_out;
+  int32_t* len_out;
+  int32_t* recent_out;             // or nullptr
+  uint32_t* ticket;                // in place: Workspace::moved
+  uint32_t* flags;
+  int32_t flag_stride;
+  int32_t same_rows;               // in place: source and target row r are the same memory
+  int32_t w_in_rows, w_out_rows;
+  int32_t B, Hkv, n_sink, recent, budget, n_chunks;
+  int32_t* guard;
+};
+
+// Dense attention of a batch that shares its first rows.
+struct SharedArgs {
+  const uint16_t* q;
+  const uint16_t* K;
+  const uint16_t* V;
+  int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  const int32_t* ctx_len;
+  const int32_t* shared_len;
+  float* part;                   // records: splits [0, n_shared) of the shared rows, [n_shared, n_shared + n_own) of a sequence's own
+  const int32_t* table;          // paged cache (see AttnArgs)
+  int64_t table_stride;
+  int32_t page_lg, page_rpb, n_blocks;
+  int32_t B, Hq, Hkv, G, lead, max_shared, len_cap, n_shared, n_own;
+  float scale_log2;
+  int32_t* guard;
+};
+
 struct MergeArgs {
   const float* part;
   float* out;
@@ -264,11 +339,20 @@ struct SelArgs {
   unsigned long long* met_out;  //   ... Workspace::met_out
   const uint32_t* wg_hist;  //   ... Workspace::wg_hist (mode 0)
   const double* wg_stat;   //   ... Workspace::wg_stat (full Selector)
+  // eviction and attention with running weights
+  const float* weights;    // [B*Hkv][w_rows]
+  float* w_out;            // the same shape
+  int32_t w_rows;
+  float decay;
+  uint32_t* moved;         // Workspace::moved, cleared by the launch that reads the weights; nullptr: not
+  int32_t moved_words;
+  int32_t* guard;          // ... which reports a ctx_len that had to be clamped here
   int32_t place_x;         // the launch's segments lie along the grid's first index, not its second (set by the launch)
   int32_t n_place;         //   ... how many of them it has
 };
 
-hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s);
+// rounded: logits exposed (no key norms), the weights' two terms to nearest
+hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool rounded = false);
 hipError_t launch_attn_evidence(const AttnArgs& a, int B, int n_slots, hipStream_t s);  // a query of a window: logits and statistics of J
 hipError_t launch_attn_dense_floor(const AttnArgs& a, int B, int n_slots, int wide, int idle_units, int writer, hipStream_t s);
 hipError_t launch_attn_ragged(const AttnArgs& d, const AttnArgs& f, bool balanced, hipStream_t s);  // d: planned dense, f: gather or compact
@@ -283,9 +367,17 @@ hipError_t launch_sel_accum(SelArgs a, int B, int nJ, hipStream_t s);
 hipError_t launch_sel_finalize(SelArgs a, int B, int nJ, hipStream_t s);
 hipError_t launch_sel_full(SelArgs a, int B, int nJ, bool hist, hipStream_t s);
 bool sel_pick_scores(int nJ, int G, int pairs, int n_cu);  // whether the selecting workgroup also scores (src 1)
-hipError_t launch_sel_pick(SelArgs a, int B, int nJ, int src, hipStream_t s);  // src 0: keys, 1: logits, 2: window evidence
+hipError_t launch_sel_pick(SelArgs a, int B, int nJ, int src, hipStream_t s);  // src 0: keys, 1: logits, 2: window evidence, 3: running weights
 hipError_t launch_sel_cand(SelArgs a, int B, int nJ, hipStream_t s);
 hipError_t launch_sel_write(SelArgs a, int B, int nJ, hipStream_t s);
+hipError_t launch_sel_weigh(SelArgs a, int B, int max_len, hipStream_t s);  // running weights += the group's mean softmax
+hipError_t launch_sel_weights(SelArgs a, int B, int nJ, hipStream_t s);     // keys and histograms from running weights (long J)
+int shared_cols(int n_cols);  // columns (sequence, query head of the group) a workgroup of the shared rows takes, of n_cols
+hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s);
+hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s);
+hipError_t launch_rope_table(const RopeTable& t, uint64_t* table, hipStream_t s);
+hipError_t launch_rope_append(const RopeArgs& a, int n_cu, hipStream_t s);
+hipError_t launch_move_rows(const MoveArgs& a, bool in_place, hipStream_t s);
 hipError_t launch_trigger(const int32_t* last_token, const uint32_t* bitmap, int vocab, int t_max, int32_t* since_slow,
                           uint8_t* is_slow, int B, hipStream_t s);
 hipError_t launch_advance(int32_t* ctx_len, int32_t* recent_start, int B, int n_sink, int recent, hipStream_t s);

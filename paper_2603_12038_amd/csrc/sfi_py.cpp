@@ -81,7 +81,8 @@ void* to_stream(PyObject* o) {
 template <typename T>
 T convert(PyObject* o, bool stream) {
   if (PyErr_Occurred() != nullptr) return T{};
-  if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>(stream ? to_stream(o) : to_pointer(o));
+  if constexpr (std::is_floating_point_v<T>) return static_cast<T>(PyFloat_AsDouble(o));
+  else if constexpr (std::is_pointer_v<T>) return reinterpret_cast<T>(stream ? to_stream(o) : to_pointer(o));
   else return static_cast<T>(to_word(o));
 }
 
@@ -112,7 +113,8 @@ PyObject* call(int (*fn)(P...), const char* where, PyObject* const* args, Py_ssi
 #define HOT_CALLS(X)                                                                                                     \
   X(sfi_slow_step) X(sfi_slow_attn) X(sfi_slow_select) X(sfi_evidence_add) X(sfi_evidence_add_causal)                     \
   X(sfi_evidence_select) X(sfi_dense_attn) X(sfi_fast_step) X(sfi_fast_step_static) X(sfi_reorg) X(sfi_fast_step_compact) \
-  X(sfi_mixed_step) X(sfi_mixed_step_compact) X(sfi_step_begin) X(sfi_mixed_step_desc) X(sfi_trigger) X(sfi_advance)
+  X(sfi_mixed_step) X(sfi_mixed_step_compact) X(sfi_step_begin) X(sfi_mixed_step_desc) X(sfi_trigger) X(sfi_advance) \
+  X(sfi_rope_append) X(sfi_shared_attn) X(sfi_weight_attn) X(sfi_evict)
 
 // The entry points, handed over by bind: this module is not linked to libsfi, so it works on the very library that
 // binding.py has loaded, wherever the package lies and whatever other copies of it are in the process.

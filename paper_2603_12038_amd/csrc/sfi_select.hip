@@ -346,6 +346,88 @@ __global__ __launch_bounds__(kSelThreads) void sel_finalize_kernel(const SelArgs
   seg_hist(a, c.bh, seg)[tid] = s_hist[tid];
 }
 
+// ---- running weights (eviction by accumulated attention weight) ------------------------------------------
+// A weight's ranking key: its bit pattern, which orders like the value; what is not above zero (a negative, NaN) counts as zero.
+__device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
+// What the launch behind the selecting ones needs, left by the first that reads the weights: the length as it was read (the
+// caller's ctx_len is overwritten in that launch), and its counters at zero.
+__device__ __forceinline__ void note_weights(const SelArgs& a, const Cell& c, int tid, int first, int step) {
+  if (first == 0 && tid == 0) {
+    const int L = min(max(c.L_in, 0), a.len_cap);
+    a.state[(int64_t)c.bh * kStateWords + ST_LEN] = (uint32_t)L;
+    if (L != c.L_in && a.guard != nullptr) atomicOr(a.guard, kGuardCtxLen);
+  }
+  if (a.moved == nullptr) return;
+  const int per = (a.moved_words + (int)(gridDim.z * a.Hkv) - 1) / (int)(gridDim.z * a.Hkv);
+  for (int i = first + tid; i < per; i += step)
+    if (c.bh * per + i < a.moved_words) a.moved[c.bh * per + i] = 0u;
+}
+// Keys and histograms of a long J.
+__global__ __launch_bounds__(kSelThreads) void sel_weights_kernel(const SelArgs a) {
+  ask(a);
+  const Place place = place_of(a);
+  const int seg = place.i, tid = threadIdx.x;
+  const Cell c = cell_of<false>(a, blockIdx.z, place.head);
+  const int p_lo = seg * kSelSeg;
+  const int nJ = nJ_of(a, c);
+  note_weights(a, c, tid, seg * kSelThreads, place.n * kSelThreads);
+  if (p_lo >= nJ) return;
+  __shared__ uint32_t s_hist[kHistBins / 2];
+  uint32_t* keys = a.keys + (int64_t)c.bh * a.ld_pos;
+  const float* w = a.weights + (int64_t)c.bh * a.w_rows + a.n_sink;
+  s_hist[tid] = 0u;
+  uint32_t k[2][4];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p_lo + r * (kSelSeg / 2) + tid * 4 + i;
+      k[r][i] = p < nJ ? weight_key(w[p]) : 0u;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int p = p_lo + r * (kSelSeg / 2) + tid * 4;
+    if (p >= nJ) continue;
+    *reinterpret_cast<uint4*>(keys + p) = make_uint4(k[r][0], k[r][1], k[r][2], k[r][3]);
+    hist_add4(s_hist, k[r], p, nJ);
+  }
+  __syncthreads();
+  seg_hist(a, c.bh, seg)[tid] = s_hist[tid];
+}
+// Behind a dense launch that exposed the logits of all rows: w_out = decay * weights + (1 / G) sum over the heads of the softmax,
+// 1024 rows per workgroup; the last G workgroups of a pair merge the dense records into the output, as in the scoring launch.
+template <int GT>
+__global__ __launch_bounds__(kSelThreads) void sel_weigh_kernel(const SelArgs a) {
+  ask(a);
+  const Place place = place_of(a);
+  const int seg = place.i, tid = threadIdx.x;
+  const Cell c = cell_of<false>(a, blockIdx.z, place.head);
+  if (seg >= place.n - a.G) {  // workgroup-uniform
+    merge_head(a, c, seg - (place.n - a.G));
+    return;
+  }
+  __shared__ float s_jM[GT], s_jc[GT];
+  const int p = seg * 1024 + tid * 4;
+  const int L = min(max(c.L_in, 0), a.len_cap);
+  const int pq[1] = {p};
+  float4 lq[1][GT];
+  request_logits<1, GT>(lq, a.logits + (int64_t)c.bh * a.lg_rows * a.ld_pos, a.lg_rows, a.G, pq);
+  const int64_t at = (int64_t)c.bh * a.w_rows + p;
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.weights != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = p + i < L ? a.weights[at + i] : 0.f;
+  }
+  group_stats<GT>(a, c, kSelThreads / 64, s_jM, s_jc);
+  __syncthreads();
+  float f[1][4];
+  evidence<1, GT>(f, lq, 1.0f, s_jM, s_jc);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (p + i < L) a.w_out[at + i] = a.weights != nullptr ? a.decay * w[i] + f[0][i] : f[0][i];
+}
+
 // ---- full Selector (mode 1): two kernels in place of the scoring --------------------------------------
 // All scores of this part live in the log2 domain, Z = log2(s + eps) = z / ln 2: Soft-NMS is
 // homogeneous of degree one in z, the head softmax of z / T is 2^(Z / T) normalised, and the
@@ -577,7 +659,7 @@ __global__ __launch_bounds__(kFuseThreads) void sel_fuse_kernel(const SelArgs a)
 
 // ---- short J: one workgroup per pair selects --------------------------------------------------------
 // SRC 0: the keys a scoring launch left; 1: straight from the logits (scoring included; workgroups of places > 0 merge the
-// dense records, four query heads each); 2: the accumulated evidence of a window.
+// dense records, four query heads each); 2: the accumulated evidence of a window; 3: running weights.
 // A thread holds P consecutive positions in registers.  The three radix passes run on LDS histograms over all of J;
 // no list of candidates, no global histogram.
 template <int P, int SRC, bool LIST, int GT>
@@ -618,6 +700,13 @@ __global__ __launch_bounds__(kPickThreads) void sel_pick_kernel(const SelArgs a)
       if (p0 < nJ) evidence<NQ, GT>(f, lq, a.alpha, s_jM, s_jc);
 #pragma unroll
       for (int i = 0; i < P; ++i) key[i] = p0 + i < nJ ? __float_as_uint(f[i / 4][i % 4]) : 0u;
+    } else if (SRC == 3) {
+      const float* w = a.weights + (int64_t)c.bh * a.w_rows + a.n_sink + p0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) key[i] = p0 + i < nJ ? weight_key(w[i]) : 0u;
+      note_weights(a, c, tid, place.i * kPickThreads, kPickThreads);
+      for (int i = tid; i < (4096 + 1024 + 512) / 4; i += kPickThreads) reinterpret_cast<uint4*>(s_h)[i] = make_uint4(0u, 0u, 0u, 0u);
+      __syncthreads();
     } else {
       const uint32_t* src = (SRC == 0 ? a.keys : reinterpret_cast<const uint32_t*>(a.mu)) + (int64_t)c.bh * a.ld_pos;
 #pragma unroll
@@ -1084,6 +1173,21 @@ hipError_t launch_sel_finalize(SelArgs a, int B, int nJ, hipStream_t s) {
   hipLaunchKernelGGL(sel_finalize_kernel, grid, dim3(kSelThreads), 0, s, a);
   return hipGetLastError();
 }
+hipError_t launch_sel_weights(SelArgs a, int B, int nJ, hipStream_t s) {
+  const dim3 grid = place_grid(&a, ceil_seg(nJ, kSelSeg), B);
+  hipLaunchKernelGGL(sel_weights_kernel, grid, dim3(kSelThreads), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t launch_sel_weigh(SelArgs a, int B, int max_len, hipStream_t s) {
+  const dim3 grid = place_grid(&a, ceil_seg(max_len, 1024) + a.G, B), block(kSelThreads);
+  if (a.G <= 1) hipLaunchKernelGGL(sel_weigh_kernel<1>, grid, block, 0, s, a);
+  else if (a.G <= 2) hipLaunchKernelGGL(sel_weigh_kernel<2>, grid, block, 0, s, a);
+  else if (a.G <= 4) hipLaunchKernelGGL(sel_weigh_kernel<4>, grid, block, 0, s, a);
+  else if (a.G <= 5) hipLaunchKernelGGL(sel_weigh_kernel<5>, grid, block, 0, s, a);
+  else if (a.G <= 8) hipLaunchKernelGGL(sel_weigh_kernel<8>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(sel_weigh_kernel<16>, grid, block, 0, s, a);
+  return hipGetLastError();
+}
 template <bool FROM_MU, bool LIST, bool FLAGS>
 static void launch_prior_t(const SelArgs& a, dim3 grid, hipStream_t s) {
   const dim3 block(kSelThreads);
@@ -1158,6 +1262,8 @@ hipError_t launch_sel_pick(SelArgs a, int B, int nJ, int src, hipStream_t s) {
     }
   } else if (src == 2) {
     launch_pick_keys_t<2, false>(a, nJ, grid, s);
+  } else if (src == 3) {
+    launch_pick_keys_t<3, false>(a, nJ, grid, s);
   } else {
     if (list) launch_pick_keys_t<0, true>(a, nJ, grid, s);
     else launch_pick_keys_t<0, false>(a, nJ, grid, s);
