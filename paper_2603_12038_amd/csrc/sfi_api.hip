@@ -1436,13 +1436,13 @@ void all_rows_view(const sfi_ctx* x, sfi_ctx* y) {
 // Splits of the shared rows (none where nothing can be shared) and of each sequence's own.
 void shared_splits(const sfi_ctx* x, SharedArgs* a) {
   const int cols = shared_cols(a->B * a->G), groups = (a->B * a->G + cols - 1) / cols;
-  auto splits = [&](int tiles, int64_t cells, int cap) {
-    int64_t s = x->n_cu / cells;
+  auto splits = [&](int tiles, int64_t cells, int wgs, int cap) {
+    int64_t s = wgs / cells;
     s = std::min<int64_t>(s, (tiles + kWaves - 1) / kWaves);
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, cap));
   };
-  a->n_shared = a->max_shared > 0 ? splits((a->max_shared + kTile - 1) / kTile, (int64_t)a->Hkv * groups, 40) : 0;
-  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 20);
+  a->n_shared = a->max_shared > 0 ? splits((a->max_shared + kTile - 1) / kTile, (int64_t)a->Hkv * groups, x->n_cu, 40) : 0;
+  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 2 * x->n_cu, 20);
 }
 }  // namespace
 

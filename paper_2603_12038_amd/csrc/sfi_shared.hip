@@ -21,6 +21,8 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 namespace {
 
@@ -113,63 +115,71 @@ struct Cols {
   float m[NCB], l[NCB];  // l: of this lane's rows
   int lo[NCB], hi[NCB];  // rows this column sees
 };
-// The running maximum is let lag behind by up to kLag octaves before accumulators are rescaled (weights up to 2^kLag: nothing is lost in fp32).
+// One tile.  The products of all blocks of columns first, then their weights, then the products with V: nothing between them but one branch, so that
+// matrix and vector instructions of different blocks overlap.  The running maximum may lag behind by up to kLag octaves before
+// accumulators are rescaled (weights up to 2^kLag lose nothing in fp32), so a lane only has to look at its own rows; c2 > 0.
 constexpr float kLag = 8.f;
-template <int NCB>
-__device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const bf16x8 (&kb)[4], const bf16x8 (&vt)[8], int r0, int jg, bool masked,
-                                     float c2) {
+template <int NCB, bool MASKED>
+__device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const bf16x8 (&kb)[4], const bf16x8 (&vt)[8], int r0, int jg, float c2) {
+  f32x4 s[NCB][2];
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
-    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      s[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[k], C.q[cb][k], s[0], 0, 0, 0);
-      s[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[k], C.q[cb][k], s[1], 0, 0, 0);
+      s[cb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[k], C.q[cb][k], s[cb][0], 0, 0, 0);
+      s[cb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[k], C.q[cb][k], s[cb][1], 0, 0, 0);
     }
-    float y[8];
+  }
+  float mx[NCB];
+  bool up = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = s[i >> 2][i & 3] * c2;
-    if (masked) {
+  for (int cb = 0; cb < NCB; ++cb) {
+    if (MASKED) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int r = r0 + 16 * (i >> 2) + 4 * jg + (i & 3);
-        y[i] = r >= C.lo[cb] && r < C.hi[cb] ? y[i] : kNeg;
+        s[cb][i >> 2][i & 3] = r >= C.lo[cb] && r < C.hi[cb] ? s[cb][i >> 2][i & 3] : -__builtin_inff();
       }
     }
-    float mx = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-    mx = across_max(mx);
-    if (__any(mx > C.m[cb] + kLag)) {
-      const float m1 = fmaxf(mx, C.m[cb]);
+    mx[cb] = fmaxf(fmaxf(fmaxf(s[cb][0][0], s[cb][0][1]), fmaxf(s[cb][0][2], s[cb][0][3])),
+                   fmaxf(fmaxf(s[cb][1][0], s[cb][1][1]), fmaxf(s[cb][1][2], s[cb][1][3]))) * c2;
+    up |= mx[cb] > C.m[cb] + kLag;
+  }
+  if (__any(up)) {
+#pragma unroll
+    for (int cb = 0; cb < NCB; ++cb) {
+      const float m1 = fmaxf(across_max(mx[cb]), C.m[cb]);  // (not below kNeg: finite)
       const float f = __builtin_amdgcn_exp2f(C.m[cb] - m1);
       C.m[cb] = m1;
       C.l[cb] *= f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
     }
-    float p[8], rest[8];
+  }
+  bf16x8 ph[NCB], pl[NCB];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(y[i] - C.m[cb]);
-    if (masked) {
+  for (int cb = 0; cb < NCB; ++cb) {
+    float p[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = y[i] == kNeg ? 0.f : p[i];
-    }
+    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[cb][i >> 2][i & 3], c2, -C.m[cb]));  // a masked row: 2^-inf = 0
     C.l[cb] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       hi[i] = round2(p[2 * i], p[2 * i + 1]);
-      rest[2 * i] = p[2 * i] - __uint_as_float(hi[i] << 16);
-      rest[2 * i + 1] = p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u);
-      lo[i] = round2(rest[2 * i], rest[2 * i + 1]);
+      lo[i] = round2(p[2 * i] - __uint_as_float(hi[i] << 16), p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
     }
-    const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], ph, C.acc[cb][e], 0, 0, 0);
-      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], pl, C.acc[cb][e], 0, 0, 0);
-    }
+    ph[cb] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    pl[cb] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int cb = 0; cb < NCB; ++cb) {
+      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], ph[cb], C.acc[cb][e], 0, 0, 0);
+      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], pl[cb], C.acc[cb][e], 0, 0, 0);
+    }
 }
 template <int NCB>
 __device__ __forceinline__ void start(Cols<NCB>& C) {
@@ -205,78 +215,87 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
     }
     turn_v(T.v, vt);
     if (t + kWaves < t1) issue<PAGED>(T, R, (t + kWaves) * kTile, jg, n, bad);
-    step<NCB>(C, ka, kb, vt, t * kTile, jg, t * kTile < whole_from || (t + 1) * kTile > whole_to, c2);
+    if (t * kTile >= whole_from && (t + 1) * kTile <= whole_to) step<NCB, false>(C, ka, kb, vt, t * kTile, jg, c2);
+    else step<NCB, true>(C, ka, kb, vt, t * kTile, jg, c2);
   }
 }
 
-// The four waves' columns joined and written as one record each: rows(col) gives the record's address, nullptr: no such column.
-template <int NCB, typename F>
-__device__ __forceinline__ void join(Cols<NCB>& C, int wave, int jg, int n, float* lds, F record) {
-  constexpr int kCols = 16 * NCB, kPitch = kHeadDim + 4;
-  float* s_m = lds;                      // [kWaves][kCols]
-  float* s_l = lds + kWaves * kCols;
-  float* s_acc = lds + 2 * kWaves * kCols;  // [2][kCols][kPitch]
-#pragma unroll
-  for (int cb = 0; cb < NCB; ++cb) {
-    const float l = across_sum(C.l[cb]);
-    if (jg == 0) {
-      s_m[wave * kCols + 16 * cb + n] = C.m[cb];
-      s_l[wave * kCols + 16 * cb + n] = l;
-    }
-  }
-  __syncthreads();
+// Joins the columns of the NR waves that had other rows of the same columns (rank: which of them this wave is, 0 .. NR - 1; cols: the columns of all
+// of the workgroup's waves, c0: this wave's first) and writes them as one record each: record(col) gives its address, nullptr: no such column.
+// lds: join_floats.
+template <int NR>
+constexpr int join_floats(int cols) { return 2 * NR * cols + (NR > 1 ? NR / 2 * cols * (kHeadDim + 4) : 0); }
+template <int NCB, int NR, bool TURNED, typename F>
+__device__ __forceinline__ void join(Cols<NCB>& C, int rank, int cols, int c0, int jg, int n, float* lds, F record) {
+  constexpr int kPitch = kHeadDim + 4;
   float M[NCB], Z[NCB];
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
-    const int c = 16 * cb + n;
-    M[cb] = fmaxf(fmaxf(s_m[c], s_m[kCols + c]), fmaxf(s_m[2 * kCols + c], s_m[3 * kCols + c]));
-    Z[cb] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) Z[cb] += s_l[w * kCols + c] * __builtin_amdgcn_exp2f(s_m[w * kCols + c] - M[cb]);
-    const float f = __builtin_amdgcn_exp2f(C.m[cb] - M[cb]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
+    M[cb] = C.m[cb];
+    Z[cb] = across_sum(C.l[cb]);
   }
-  for (int left = kWaves / 2; left >= 1; left >>= 1) {  // the upper half hands over to the lower one
-    if (wave >= left && wave < 2 * left) {
+  if (NR > 1) {
+    float* s_m = lds;               // [NR][cols]
+    float* s_l = lds + NR * cols;
+    float* s_acc = lds + 2 * NR * cols;  // [NR / 2][cols][kPitch]
 #pragma unroll
-      for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float* p = s_acc + ((wave - left) * kCols + 16 * cb + n) * kPitch + 8 * (4 * jg + i);
-          *reinterpret_cast<float4*>(p) = make_float4(C.acc[cb][0][i], C.acc[cb][1][i], C.acc[cb][2][i], C.acc[cb][3][i]);
-          *reinterpret_cast<float4*>(p + 4) = make_float4(C.acc[cb][4][i], C.acc[cb][5][i], C.acc[cb][6][i], C.acc[cb][7][i]);
-        }
-    }
+    for (int cb = 0; cb < NCB; ++cb)
+      if (jg == 0) {
+        s_m[rank * cols + c0 + 16 * cb + n] = C.m[cb];
+        s_l[rank * cols + c0 + 16 * cb + n] = Z[cb];
+      }
     __syncthreads();
-    if (wave < left) {
 #pragma unroll
-      for (int cb = 0; cb < NCB; ++cb)
+    for (int cb = 0; cb < NCB; ++cb) {
+      const int c = c0 + 16 * cb + n;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float* p = s_acc + (wave * kCols + 16 * cb + n) * kPitch + 8 * (4 * jg + i);
+      for (int w = 0; w < NR; ++w) M[cb] = fmaxf(M[cb], s_m[w * cols + c]);
+      Z[cb] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) C.acc[cb][e][i] += p[e];
-        }
+      for (int w = 0; w < NR; ++w) Z[cb] += s_l[w * cols + c] * __builtin_amdgcn_exp2f(s_m[w * cols + c] - M[cb]);
+      const float f = __builtin_amdgcn_exp2f(C.m[cb] - M[cb]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
     }
-    __syncthreads();
+#pragma unroll
+    for (int left = NR / 2; left >= 1; left >>= 1) {  // the upper half hands over to the lower one
+      if (rank >= left && rank < 2 * left) {
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<f32x4*>(s_acc + ((rank - left) * cols + c0 + 16 * cb + n) * kPitch + 16 * e + 4 * jg) = C.acc[cb][e];
+      }
+      __syncthreads();
+      if (rank < left) {
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            C.acc[cb][e] += *reinterpret_cast<const f32x4*>(s_acc + (rank * cols + c0 + 16 * cb + n) * kPitch + 16 * e + 4 * jg);
+      }
+      if (left > 1) __syncthreads();
+    }
   }
-  if (wave != 0) return;
+  if (rank != 0) return;
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
-    float* rec = record(16 * cb + n);
+    float* rec = record(c0 + 16 * cb + n);
     if (rec == nullptr) continue;
     if (jg == 0) *reinterpret_cast<float4*>(rec) = make_float4(M[cb], Z[cb], kNeg, 0.f);
+    if (TURNED) {  // acc[e][i]: dim 8 (4 jg + i) + e
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float4* p = reinterpret_cast<float4*>(rec + 4 + 8 * (4 * jg + i));
-      p[0] = make_float4(C.acc[cb][0][i], C.acc[cb][1][i], C.acc[cb][2][i], C.acc[cb][3][i]);
-      p[1] = make_float4(C.acc[cb][4][i], C.acc[cb][5][i], C.acc[cb][6][i], C.acc[cb][7][i]);
+      for (int i = 0; i < 4; ++i) {
+        float4* p = reinterpret_cast<float4*>(rec + 4 + 8 * (4 * jg + i));
+        p[0] = make_float4(C.acc[cb][0][i], C.acc[cb][1][i], C.acc[cb][2][i], C.acc[cb][3][i]);
+        p[1] = make_float4(C.acc[cb][4][i], C.acc[cb][5][i], C.acc[cb][6][i], C.acc[cb][7][i]);
+      }
+    } else {  // dim 16 e + 4 jg + i
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *reinterpret_cast<f32x4*>(rec + 4 + 16 * e + 4 * jg) = C.acc[cb][e];
     }
   }
 }
-template <int NCB>
-constexpr int join_floats() { return 2 * kWaves * 16 * NCB + 2 * 16 * NCB * (kHeadDim + 4); }
 
 __device__ __forceinline__ Rows rows_of(const SharedArgs& a, int b, int h) {
   Rows R;
@@ -297,91 +316,193 @@ __device__ __forceinline__ int shared_of(const SharedArgs& a, int b, int L, int 
   return min(max(a.shared_len[b], 0), min(min(L, L_lead), a.max_shared));
 }
 
-// The shared rows: a workgroup per KV head, split and group of 16 NCB columns (column c = query head c % G of the KV head's group in sequence c / G).
-template <int NCB, bool PAGED>
-__global__ __launch_bounds__(kAttnThreads, 1) void shared_rows_kernel(const SharedArgs a) {
-  __shared__ __align__(16) float lds[join_floats<NCB>()];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
-  const int h = blockIdx.x, split = blockIdx.y, c0 = blockIdx.z * (16 * NCB);
-  const int n_cols = a.B * a.G;
-  const int L_lead = len_of(a, a.lead);
-  Cols<NCB> C;
-  start(C);
+// What a workgroup's columns are: column c = query head c % G of the KV head's group in sequence c / G, and how many of the lead's rows it sees.
+struct Seen {
+  int most, least;  // over the wave's columns
+};
+template <int NCB>
+__device__ __forceinline__ Seen load_columns(const SharedArgs& a, Cols<NCB>& C, int c0, int h, int jg, int n) {
+  const int n_cols = a.B * a.G, L_lead = len_of(a, a.lead);
   int most = 0, least = 0x7fffffff;
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
     const int c = c0 + 16 * cb + n, cc = min(c, n_cols - 1), b = cc / a.G, g = cc % a.G;
+    load_query(C.q[cb], a.q + ((int64_t)b * a.Hq + h * a.G + g) * kHeadDim, c < n_cols, jg);
     C.lo[cb] = 0;
     C.hi[cb] = c < n_cols ? shared_of(a, b, len_of(a, b), L_lead) : 0;
     most = max(most, C.hi[cb]);
     least = min(least, c < n_cols ? C.hi[cb] : 0x7fffffff);
-    load_query(C.q[cb], a.q + ((int64_t)b * a.Hq + h * a.G + g) * kHeadDim, c < n_cols, jg);
   }
 #pragma unroll
   for (int d = 8; d >= 1; d >>= 1) {
     most = max(most, __shfl_xor(most, d));
     least = min(least, __shfl_xor(least, d));
   }
+  return {__builtin_amdgcn_readfirstlane(most), __builtin_amdgcn_readfirstlane(least)};
+}
+__device__ __forceinline__ float* shared_record(const SharedArgs& a, int c, int h, int split) {
+  return c < a.B * a.G ? a.part + (((int64_t)(c / a.G) * a.Hq + h * a.G + c % a.G) * kSlotCap + split) * kPartStride : nullptr;
+}
+
+// The shared rows for few columns (16 NCB in all): a workgroup per KV head and split, every wave with rows of its own in registers.
+template <int NCB, bool PAGED>
+__global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const SharedArgs a) {
+  __shared__ __align__(16) float lds[join_floats<kWaves>(16 * NCB)];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
+  const int h = blockIdx.x, split = blockIdx.y;
+  Cols<NCB> C;
+  start(C);
+  const Seen seen = load_columns(a, C, 0, h, jg, n);
+  int bad = 0;
+  if (seen.most > 0) {
+    Rows R = rows_of(a, a.lead, h);
+    R.hi = seen.most - 1;
+    const int tiles = (seen.most + kTile - 1) / kTile;
+    walk<NCB, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, seen.least, wave, jg, n, a.scale_log2, bad);
+  }
+  join<NCB, kWaves, true>(C, wave, 16 * NCB, 0, jg, n, lds, [&](int col) { return shared_record(a, col, h, split); });
+  if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
+}
+
+// The shared rows for many columns: the tiles go through LDS, where all waves of the workgroup read them.  CG groups of 16 NCB columns,
+// and RG groups of waves that take a tile each of a stage of RG tiles.  Every thread requests kAhead stages in front (64 KB a compute unit
+// on their way), as 16 bytes of a row each, and stores a stage into one of two buffers while the other is read: one barrier per stage.
+// In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read together,
+// one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of four rows),
+// lies in different banks.
+template <int NCB, int CG, int RG, bool PAGED>
+__global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
+  constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
+  constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
+  constexpr int kRowStep = kThreads / 16;
+  constexpr int kAhead = CG >= 8 ? 2 : 4 / kLoads;
+  static_assert(kLoads * kThreads == kRowsHere * 16 && kAhead >= 1, "whole rounds");
+  constexpr int kStage = kRowsHere * 512;
+  constexpr int kLds = 2 * kStage > 4 * join_floats<RG>(kCols) ? 2 * kStage : 4 * join_floats<RG>(kCols);
+  __shared__ __align__(16) unsigned char lds[kLds];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, jg = lane >> 4, n = lane & 15;
+  const int cg = wave % CG, rg = wave / CG;
+  const int h = blockIdx.x, split = blockIdx.y, c_first = blockIdx.z * kCols, c0 = 16 * NCB * cg;
+  __shared__ int s_most[CG * RG];
+  Cols<NCB> C;
+  start(C);
+  const Seen seen = load_columns(a, C, c_first + c0, h, jg, n);
+  if (lane == 0) s_most[wave] = seen.most;
+  __syncthreads();
+  int most = 0;
+#pragma unroll
+  for (int w = 0; w < CG; ++w) most = max(most, s_most[w]);
   most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
   int bad = 0;
   if (most > 0) {
-    Rows R = rows_of(a, a.lead, h);
-    R.hi = most - 1;
-    const int tiles = (most + kTile - 1) / kTile;
-    walk<NCB, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, least, wave, jg, n, a.scale_log2, bad);
+    const Rows R = rows_of(a, a.lead, h);
+    const int last = most - 1;
+    const int stages = (most + kRowsHere - 1) / kRowsHere;
+    const int t0 = (int)((int64_t)stages * split / a.n_shared), t1 = (int)((int64_t)stages * (split + 1) / a.n_shared);
+    const int my_row = tid >> 4, piece = tid & 15;
+    uint4 pk[kAhead][kLoads], pv[kAhead][kLoads];
+    auto request = [&](int slot, int t) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int row = min(t * kRowsHere + my_row + j * kRowStep, last);
+        uint32_t at = (uint32_t)row;
+        if (PAGED) {
+          const int page = R.table[row >> R.lg], pc = min(max(page, 0), R.n_blocks - 1);
+          bad |= pc != page ? kGuardBlock : 0;
+          at = (uint32_t)(pc * R.rpb + (row & ((1 << R.lg) - 1)));
+        }
+        pk[slot][j] = load16(R.K + (uint64_t)at * R.k_st + piece * 16);
+        pv[slot][j] = load16(R.V + (uint64_t)at * R.v_st + piece * 16);
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+      if (t0 + s < t1) request(s, t0 + s);
+    const unsigned char* k_at = lds + (rg * kTile + n) * 256;
+    const unsigned char* v_at = lds + kRowsHere * 256 + (rg * kTile + 4 * jg + (n >> 2)) * 256 + 8 * (n & 3);
+    const int v_turn = (4 * jg + (n >> 2)) & 7;
+    for (int t = t0; t < t1; t += kAhead) {
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        if (t + s >= t1) break;
+        const int buf = ((t + s - t0) & 1) * kStage;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const int r = my_row + j * kRowStep;
+          *reinterpret_cast<uint4*>(lds + buf + r * 256 + ((piece ^ (r & 15)) << 4)) = pk[s][j];
+          *reinterpret_cast<uint4*>(lds + buf + kRowsHere * 256 + r * 256 + (((piece >> 1) ^ (r & 7)) << 5) + ((piece & 1) << 4)) = pv[s][j];
+        }
+        if (t + s + kAhead < t1) request(s, t + s + kAhead);
+        __syncthreads();
+        const int r0 = (t + s) * kRowsHere + rg * kTile;
+        bf16x8 ka[4], kb[4], vt[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          ka[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + (((4 * k + jg) ^ n) << 4));
+          kb[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + 16 * 256 + (((4 * k + jg) ^ n) << 4));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const unsigned char* p = v_at + buf + ((e ^ v_turn) << 5);
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * 256));
+          vt[e] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        if (r0 + kTile <= seen.least) step<NCB, false>(C, ka, kb, vt, r0, jg, a.scale_log2);
+        else step<NCB, true>(C, ka, kb, vt, r0, jg, a.scale_log2);
+      }
+    }
   }
-  join<NCB>(C, wave, jg, n, lds, [&](int col) -> float* {
-    const int c = c0 + col;
-    if (c >= n_cols) return nullptr;
-    return a.part + (((int64_t)(c / a.G) * a.Hq + h * a.G + c % a.G) * kSlotCap + split) * kPartStride;
-  });
+  if (RG > 1) __syncthreads();  // the buffers are read no more
+  join<NCB, RG, false>(C, rg, kCols, c0, jg, n, reinterpret_cast<float*>(lds), [&](int col) { return shared_record(a, c_first + col, h, split); });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
 // A sequence's own rows: a workgroup per KV head, split and sequence.
 template <bool PAGED>
 __global__ __launch_bounds__(kAttnThreads, 2) void own_rows_kernel(const SharedArgs a) {
-  __shared__ __align__(16) float lds[join_floats<1>()];
+  __shared__ __align__(16) float lds[join_floats<kWaves>(16)];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
   const int h = blockIdx.x, split = blockIdx.y, b = blockIdx.z;
-  const int L = len_of(a, b), S = shared_of(a, b, L, len_of(a, a.lead));
   Cols<1> C;
   start(C);
+  load_query(C.q[0], a.q + ((int64_t)b * a.Hq + h * a.G + min(n, a.G - 1)) * kHeadDim, n < a.G, jg);
+  const int L = len_of(a, b), S = shared_of(a, b, L, len_of(a, a.lead));
   C.lo[0] = S;
   C.hi[0] = L;
-  load_query(C.q[0], a.q + ((int64_t)b * a.Hq + h * a.G + min(n, a.G - 1)) * kHeadDim, n < a.G, jg);
   int bad = (a.ctx_len[b] != L ? kGuardCtxLen : 0) | (a.shared_len[b] != S ? kGuardShared : 0);
   if (S < L) {
     Rows R = rows_of(a, b, h);
     R.lo = S;
     R.hi = L - 1;
     const int first = S / kTile, tiles = (L + kTile - 1) / kTile - first;
-    walk<1, PAGED>(C, R, first + tiles * split / a.n_own, first + tiles * (split + 1) / a.n_own, S, L, wave, jg, n, a.scale_log2, bad);
+    walk<1, PAGED>(C, R, first + (int)((int64_t)tiles * split / a.n_own), first + (int)((int64_t)tiles * (split + 1) / a.n_own), S, L, wave, jg, n, a.scale_log2, bad);
   }
-  join<1>(C, wave, jg, n, lds, [&](int col) -> float* {
-    if (col >= a.G) return nullptr;
-    return a.part + (((int64_t)b * a.Hq + h * a.G + col) * kSlotCap + a.n_shared + split) * kPartStride;
+  join<1, kWaves, true>(C, wave, 16, 0, jg, n, lds, [&](int col) -> float* {
+    return col < a.G ? a.part + (((int64_t)b * a.Hq + h * a.G + col) * kSlotCap + a.n_shared + split) * kPartStride : nullptr;
   });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
-template <int NCB>
-void launch_shared_t(const SharedArgs& a, hipStream_t s) {
-  const dim3 grid(a.Hkv, a.n_shared, (a.B * a.G + 16 * NCB - 1) / (16 * NCB));
-  if (a.table != nullptr) hipLaunchKernelGGL((shared_rows_kernel<NCB, true>), grid, dim3(kAttnThreads), 0, s, a);
-  else hipLaunchKernelGGL((shared_rows_kernel<NCB, false>), grid, dim3(kAttnThreads), 0, s, a);
-}
-
 }  // namespace
 
-int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 32 ? 32 : 64; }
+#define SFI_LAUNCH_PAGED(kernel, grid, threads, ...)                                                                        \
+  do {                                                                                                                      \
+    if (a.table != nullptr) hipLaunchKernelGGL((kernel<__VA_ARGS__, true>), grid, dim3(threads), 0, s, a);                  \
+    else hipLaunchKernelGGL((kernel<__VA_ARGS__, false>), grid, dim3(threads), 0, s, a);                                    \
+  } while (0)
+
+int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 32 ? 32 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256; }
 
 hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
-  switch (shared_cols(a.B * a.G)) {
-    case 16: launch_shared_t<1>(a, s); break;
-    case 32: launch_shared_t<2>(a, s); break;
-    default: launch_shared_t<4>(a, s);
+  const int cols = shared_cols(a.B * a.G);
+  const dim3 grid(a.Hkv, a.n_shared, (a.B * a.G + cols - 1) / cols);
+  switch (cols) {
+    case 16: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 1); break;
+    case 32: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 2); break;
+    case 64: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 2, 4); break;
+    case 128: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2); break;
+    default: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1);
   }
   return hipGetLastError();
 }
