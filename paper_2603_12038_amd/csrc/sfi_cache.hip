@@ -142,7 +142,10 @@ hipError_t launch_rope_append(const RopeArgs& a, int n_cu, hipStream_t s) {
 struct MoveSpan {
   int L, sinks, kept, gone, after;  // rows before; sink rows; rows of J that stay / go; rows afterwards
   const int32_t* list;
-  __device__ __forceinline__ int source(int r) const { return r < sinks ? r : r < sinks + kept ? list[r - sinks] : r + gone; }
+  __device__ __forceinline__ int source(int r) const {  // (a word of the list is read whatever r is: several rows' reads go out together)
+    const int v = list[min(max(r - sinks, 0), max(kept - 1, 0))];
+    return r < sinks ? r : r < sinks + kept ? v : r + gone;
+  }
 };
 __device__ __forceinline__ MoveSpan span_of(const MoveArgs& a, int bh) {
   MoveSpan m;
@@ -151,26 +154,44 @@ __device__ __forceinline__ MoveSpan span_of(const MoveArgs& a, int bh) {
   m.kept = a.n_kept[bh];
   m.gone = max(0, m.L - a.recent - a.n_sink) - m.kept;
   m.after = m.L - m.gone;
-  m.list = a.kept + (int64_t)bh * a.budget;
+  m.list = a.budget > 0 ? a.kept + (int64_t)bh * a.budget : a.n_kept;
   return m;
 }
-__device__ __forceinline__ int64_t cache_row(const int32_t* table, int64_t table_stride, int lg, int rpb, int n_blocks, int b, int row, int& bad) {
-  if (table == nullptr) return row;
-  const int page = table[(int64_t)b * table_stride + (row >> lg)];
-  const int pc = min(max(page, 0), n_blocks - 1);
-  bad |= pc != page ? kGuardBlock : 0;
-  return (int64_t)pc * rpb + (row & ((1 << lg) - 1));
+// Row numbers in the cache of N logical rows of sequence b; bit i of the result: row i's block id is in the pool.
+template <int N>
+__device__ __forceinline__ unsigned rows_in_pool(int64_t (&at)[N], const int (&row)[N], const int32_t* table, int64_t table_stride, int lg, int rpb,
+                                                 int n_blocks, int b, int& bad) {
+  unsigned ok = (1u << N) - 1;
+  if (table == nullptr) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = row[i];
+    return ok;
+  }
+  int page[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) page[i] = table[(int64_t)b * table_stride + (row[i] >> lg)];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int pc = min(max(page[i], 0), n_blocks - 1);
+    if (pc != page[i]) {
+      bad |= kGuardBlock;
+      ok &= ~(1u << i);
+    }
+    at[i] = (int64_t)pc * rpb + (row[i] & ((1 << lg) - 1));
+  }
+  return ok;
 }
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kMoveThreads = 256;
 constexpr int kMoveItems = kMoveRows / (kMoveThreads / 16);
 static_assert(kMoveRows % (kMoveThreads / 16) == 0, "whole rounds of 16 lanes a row");
 
-// Workgroups [0, n_chunks * pairs): kMoveRows rows of K and V of a pair each.  The last `pairs`: a pair's weights and positions, its lengths.
+// The first `pairs` workgroups: a pair's weights and positions, its lengths (the longest way).  The others: kMoveRows rows of K and V of a pair each.
 // IN_PLACE: source and target are the same rows.  A row only ever moves down, so a chunk's target is the source of its own and
 // of lower chunks: a workgroup holds its rows in registers, says so, and stores once the lower chunks whose sources it overwrites have
 // said so.  Chunks are dealt by a counter, lower ones first, and nobody waits before having said its own: every wait ends.
-template <bool IN_PLACE>
+template <bool IN_PLACE, bool STREAM>
 __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs a) {
   const int tid = threadIdx.x;
   __shared__ int s_ticket;
@@ -181,11 +202,11 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
     unit = s_ticket;
   }
   const int pairs = a.B * a.Hkv;
-  const int bh = unit % pairs, chunk = unit / pairs;
+  const int bh = unit % pairs, chunk = unit / pairs - 1;
   const int b = bh / a.Hkv, h = bh % a.Hkv;
   const MoveSpan m = span_of(a, bh);
 
-  if (chunk == a.n_chunks) {
+  if (chunk < 0) {
     // One workgroup per pair, front to back: what it reads of a trip lies at or behind what it writes, and behind all it wrote before.
     constexpr int kPer = 8;
     const float* w_in = a.w_in + (int64_t)bh * a.w_in_rows;
@@ -227,54 +248,73 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
   if (IN_PLACE && a.same_rows && m.source(last) == last) return;  // sources ascend: nothing up to here has moved
   int bad = 0;
   const int c = tid & 15, rr = tid >> 4;
-  uint4 k4[kMoveItems], v4[kMoveItems];
+  // (rows behind the last one repeat it: no branch between the requests)
+  int from[kMoveItems];
+  int64_t src[kMoveItems];
+#pragma unroll
+  for (int i = 0; i < kMoveItems; ++i) from[i] = m.source(min(r0 + rr + i * (kMoveThreads / 16), last));
+  rows_in_pool<kMoveItems>(src, from, a.table, a.table_stride, a.page_lg, a.page_rpb, a.n_blocks, b, bad);
+  const uint16_t* Kb = a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh + 8 * c;
+  const uint16_t* Vb = a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh + 8 * c;
+  u32x4 k4[kMoveItems], v4[kMoveItems];
 #pragma unroll
   for (int i = 0; i < kMoveItems; ++i) {
-    const int r = r0 + rr + i * (kMoveThreads / 16);
-    if (r <= last) {
-      const int64_t src = cache_row(a.table, a.table_stride, a.page_lg, a.page_rpb, a.n_blocks, b, m.source(r), bad);
-      k4[i] = *reinterpret_cast<const uint4*>(a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh + src * a.k_st + 8 * c);
-      v4[i] = *reinterpret_cast<const uint4*>(a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh + src * a.v_st + 8 * c);
-    }
+    k4[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(Kb + src[i] * a.k_st));
+    v4[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(Vb + src[i] * a.v_st));
   }
+  int to[kMoveItems];
+  int64_t dst[kMoveItems];
+#pragma unroll
+  for (int i = 0; i < kMoveItems; ++i) to[i] = min(r0 + rr + i * (kMoveThreads / 16), last);
+  const unsigned ok = rows_in_pool<kMoveItems>(dst, to, a.table_out, a.table_out_stride, a.page_out_lg, a.page_out_rpb, a.n_blocks_out, b, bad);
   if (IN_PLACE) {
     // all of the workgroup's rows have arrived before it says so
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     uint32_t* flag = a.flags + (int64_t)bh * a.flag_stride;
-    if (tid == 0) {
-      __hip_atomic_store(flag + chunk, 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
-      // first kept row that lies at or behind this chunk's first target: chunks from its place on read what is overwritten here
-      int lo = 0, hi = r0;  // source(r) >= r: the answer is at most r0
+    if (tid == 0) __hip_atomic_store(flag + chunk, 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid < 64) {
+      // first row whose source lies at or behind this chunk's first target (source(r) >= r: at most r0), 64 places a trip
+      int lo = 0, hi = r0;
       while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (m.source(mid) >= r0) hi = mid;
-        else lo = mid + 1;
+        const int stride = (hi - lo + 63) / 64, at = lo + tid * stride;
+        const uint64_t from_here = __ballot(at >= hi || m.source(min(at, hi - 1)) >= r0);
+        const int f = from_here != 0ull ? __builtin_ctzll(from_here) : 64;
+        const int up = min(lo + f * stride, hi);
+        lo = f == 0 ? lo : lo + (f - 1) * stride + 1;  // the place before was too early
+        hi = f == 0 ? lo : up;
       }
-      for (int d = lo / kMoveRows; d < chunk; ++d)
-        while (__hip_atomic_load(flag + d, __ATOMIC_ACQUIRE, __HIP_MEMORY_SCOPE_AGENT) == 0u) __builtin_amdgcn_s_sleep(2);
+      // chunks from its place on have sources in what is overwritten here
+      for (int d0 = lo / kMoveRows; d0 < chunk; d0 += 64) {
+        const int d = min(d0 + tid, chunk - 1);
+        while (!__all(__hip_atomic_load(flag + d, __ATOMIC_ACQUIRE, __HIP_MEMORY_SCOPE_AGENT) != 0u)) __builtin_amdgcn_s_sleep(2);
+      }
     }
     __syncthreads();
   }
+  uint16_t* Ko = a.K_out + (int64_t)b * a.ko_sb + (int64_t)h * a.ko_sh + 8 * c;
+  uint16_t* Vo = a.V_out + (int64_t)b * a.vo_sb + (int64_t)h * a.vo_sh + 8 * c;
 #pragma unroll
-  for (int i = 0; i < kMoveItems; ++i) {
-    const int r = r0 + rr + i * (kMoveThreads / 16);
-    if (r <= last) {
-      int out_bad = 0;
-      const int64_t dst = cache_row(a.table_out, a.table_out_stride, a.page_out_lg, a.page_out_rpb, a.n_blocks_out, b, r, out_bad);
-      bad |= out_bad;
-      if (out_bad == 0) {  // a block that is not in the pool is not written
-        *reinterpret_cast<uint4*>(a.K_out + (int64_t)b * a.ko_sb + (int64_t)h * a.ko_sh + dst * a.ko_st + 8 * c) = k4[i];
-        *reinterpret_cast<uint4*>(a.V_out + (int64_t)b * a.vo_sb + (int64_t)h * a.vo_sh + dst * a.vo_st + 8 * c) = v4[i];
+  for (int i = 0; i < kMoveItems; ++i)
+    if (r0 + rr + i * (kMoveThreads / 16) <= last && (ok >> i & 1u) != 0) {  // a block that is not in the pool is not written
+      if (STREAM) {
+        __builtin_nontemporal_store(k4[i], reinterpret_cast<u32x4*>(Ko + dst[i] * a.ko_st));
+        __builtin_nontemporal_store(v4[i], reinterpret_cast<u32x4*>(Vo + dst[i] * a.vo_st));
+      } else {
+        *reinterpret_cast<u32x4*>(Ko + dst[i] * a.ko_st) = k4[i];
+        *reinterpret_cast<u32x4*>(Vo + dst[i] * a.vo_st) = v4[i];
       }
     }
-  }
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
+// Rows are read past the caches (nobody reads them again: 38 -> 32 us for 4 caches of 60000 rows cut to 4261), and written past them where
+// the new caches would not stay there for the next step anyway: 16 x 4092 rows (268 MB) 113 -> 107 us, the 4 x 4261 (70 MB) 32 -> 36.
 hipError_t launch_move_rows(const MoveArgs& a, bool in_place, hipStream_t s) {
   const dim3 grid((unsigned)(a.n_chunks + 1) * (unsigned)(a.B * a.Hkv)), block(kMoveThreads);
-  if (in_place) hipLaunchKernelGGL(move_rows_kernel<true>, grid, block, 0, s, a);
-  else hipLaunchKernelGGL(move_rows_kernel<false>, grid, block, 0, s, a);
+  const int64_t bytes = (int64_t)a.B * a.Hkv * a.n_chunks * kMoveRows * (4 * kHeadDim);
+  if (in_place) hipLaunchKernelGGL((move_rows_kernel<true, false>), grid, block, 0, s, a);
+  else if (bytes > kCacheBytes / 2) hipLaunchKernelGGL((move_rows_kernel<false, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((move_rows_kernel<false, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
