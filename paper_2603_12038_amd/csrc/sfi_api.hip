@@ -1442,7 +1442,8 @@ void shared_splits(const sfi_ctx* x, SharedArgs* a) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, cap));
   };
   a->n_shared = a->max_shared > 0 ? splits((a->max_shared + kTile - 1) / kTile, (int64_t)a->Hkv * groups, x->n_cu, 40) : 0;
-  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 2 * x->n_cu, 20);
+  // three workgroups of the own rows' launch fit a unit; a wave has a tile at least
+  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 3 * x->n_cu, 20);
 }
 }  // namespace
 
@@ -1526,10 +1527,11 @@ int sfi_shared_attn(sfi_ctx* x, const void* q, const void* K, const void* V, con
   a.scale_log2 = (float)((double)x->scale * 1.4426950408889634);
   a.guard = x->ws.guard;
   shared_splits(x, &a);
+  a.out = (float*)out;
+  a.arrive = x->ws.arrive;
+  a.out_bf16 = c.out_bf16;
   if (a.n_shared > 0) { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_shared_rows(a, st)); if (!t.stop()) return SFI_ELAUNCH; }
   { StageTimer t(x, st, SFI_STAGE_ATTN2); SFI_TRY(launch_own_rows(a, st)); if (!t.stop()) return SFI_ELAUNCH; }
-  MergeArgs m{x->ws.part, (float*)out, nullptr, c.n_q_heads, a.n_shared + a.n_own, 0, 0, nullptr, nullptr, x->G, x->alpha, c.out_bf16};
-  { StageTimer t(x, st, SFI_STAGE_MERGE); SFI_TRY(launch_merge(m, c.batch, st)); if (!t.stop()) return SFI_ELAUNCH; }
   return SFI_OK;
 }
 

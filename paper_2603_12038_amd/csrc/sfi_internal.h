@@ -277,6 +277,9 @@ struct SharedArgs {
   int32_t page_lg, page_rpb, n_blocks;
   int32_t B, Hq, Hkv, G, lead, max_shared, len_cap, n_shared, n_own;
   float scale_log2;
+  float* out;
+  uint32_t* arrive;              // Workspace::arrive: the first counter of a pair counts its workgroups of the own rows' launch
+  int32_t out_bf16;
   int32_t* guard;
 };
 
@@ -374,7 +377,7 @@ hipError_t launch_sel_weigh(SelArgs a, int B, int max_len, hipStream_t s);  // r
 hipError_t launch_sel_weights(SelArgs a, int B, int nJ, hipStream_t s);     // keys and histograms from running weights (long J)
 int shared_cols(int n_cols);  // columns (sequence, query head of the group) a workgroup of the shared rows takes, of n_cols
 hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s);
-hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s);
+hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s);  // behind launch_shared_rows: also merges
 hipError_t launch_rope_table(const RopeTable& t, uint64_t* table, hipStream_t s);
 hipError_t launch_rope_append(const RopeArgs& a, int n_cu, hipStream_t s);
 hipError_t launch_move_rows(const MoveArgs& a, bool in_place, hipStream_t s);

@@ -14,6 +14,7 @@
 // A weight goes into the second product as the sum of two bf16 (what is lost is below 2^-17 of it): with one the output would
 // carry the weights' 2^-9, with two it has fp32's accuracy but for the order of the sums.
 #include "sfi_internal.h"
+#include "sfi_wave.h"
 
 namespace sfi {
 
@@ -74,37 +75,43 @@ __device__ __forceinline__ Block block_of(const Rows& R, int r0, int& bad) {
   }
   return b;
 }
-__device__ __forceinline__ uint4 load16(const char* p) { return *reinterpret_cast<const uint4*>(p); }
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+// STREAM: past the caches, for rows that no other workgroup reads.
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const char* p) {
+  const u32x4 v = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 
 struct Tile {
   uint4 ka[4], kb[4], v[8];
 };
 template <bool PAGED>
-__device__ __forceinline__ void issue(Tile& T, const Rows& R, int r0, int jg, int n, int& bad) {
-  const Block A = block_of<PAGED>(R, r0, bad), B = block_of<PAGED>(R, r0 + 16, bad);
+__device__ __forceinline__ void issue_k(Tile& T, const Rows& R, const Block& A, const Block& B, int r0, int jg, int n) {
   const char* pa = R.K + (uint64_t)(uint32_t)(min(max(r0 + n, A.first), A.last) + A.base) * R.k_st + jg * 16;
   const char* pb = R.K + (uint64_t)(uint32_t)(min(max(r0 + 16 + n, B.first), B.last) + B.base) * R.k_st + jg * 16;
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb) {
-    T.ka[kb] = load16(pa + kb * 64);
-    T.kb[kb] = load16(pb + kb * 64);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    T.v[i] = load16(R.V + (uint64_t)(uint32_t)(min(max(r0 + 4 * jg + i, A.first), A.last) + A.base) * R.v_st + n * 16);
-    T.v[4 + i] = load16(R.V + (uint64_t)(uint32_t)(min(max(r0 + 16 + 4 * jg + i, B.first), B.last) + B.base) * R.v_st + n * 16);
+    T.ka[kb] = load16<true>(pa + kb * 64);
+    T.kb[kb] = load16<true>(pb + kb * 64);
   }
 }
-// vt[e]: element e of each of the eight rows, the operand of product e.
-__device__ __forceinline__ void turn_v(const uint4 (&v)[8], bf16x8 (&vt)[8]) {
+template <bool PAGED>
+__device__ __forceinline__ void issue_v(Tile& T, const Rows& R, const Block& A, const Block& B, int r0, int jg, int n) {
 #pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = d == 0 ? v[i].x : d == 1 ? v[i].y : d == 2 ? v[i].z : v[i].w;
-    vt[2 * d] = __builtin_bit_cast(bf16x8, make_uint4(pack_lo(w[0], w[1]), pack_lo(w[2], w[3]), pack_lo(w[4], w[5]), pack_lo(w[6], w[7])));
-    vt[2 * d + 1] = __builtin_bit_cast(bf16x8, make_uint4(pack_hi(w[0], w[1]), pack_hi(w[2], w[3]), pack_hi(w[4], w[5]), pack_hi(w[6], w[7])));
+  for (int i = 0; i < 4; ++i) {
+    T.v[i] = load16<true>(R.V + (uint64_t)(uint32_t)(min(max(r0 + 4 * jg + i, A.first), A.last) + A.base) * R.v_st + n * 16);
+    T.v[4 + i] = load16<true>(R.V + (uint64_t)(uint32_t)(min(max(r0 + 16 + 4 * jg + i, B.first), B.last) + B.base) * R.v_st + n * 16);
   }
+}
+// Element e of each of the eight rows: the operand of product e.
+__device__ __forceinline__ bf16x8 turn_v(const uint4 (&v)[8], int e) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = (e >> 1) == 0 ? v[i].x : (e >> 1) == 1 ? v[i].y : (e >> 1) == 2 ? v[i].z : v[i].w;
+  return __builtin_bit_cast(bf16x8, (e & 1) == 0 ? make_uint4(pack_lo(w[0], w[1]), pack_lo(w[2], w[3]), pack_lo(w[4], w[5]), pack_lo(w[6], w[7]))
+                                                 : make_uint4(pack_hi(w[0], w[1]), pack_hi(w[2], w[3]), pack_hi(w[4], w[5]), pack_hi(w[6], w[7])));
 }
 
 // NCB blocks of 16 columns of a wave.
@@ -115,13 +122,10 @@ struct Cols {
   float m[NCB], l[NCB];  // l: of this lane's rows
   int lo[NCB], hi[NCB];  // rows this column sees
 };
-// One tile.  The products of all blocks of columns first, then their weights, then the products with V: nothing between them but one branch, so that
-// matrix and vector instructions of different blocks overlap.  The running maximum may lag behind by up to kLag octaves before
-// accumulators are rescaled (weights up to 2^kLag lose nothing in fp32), so a lane only has to look at its own rows; c2 > 0.
-constexpr float kLag = 8.f;
-template <int NCB, bool MASKED>
-__device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const bf16x8 (&kb)[4], const bf16x8 (&vt)[8], int r0, int jg, float c2) {
-  f32x4 s[NCB][2];
+// One tile in three parts: products with K, weights, products with V.  Each does all blocks of columns, with one branch in
+// all, so that matrix and vector instructions of different blocks overlap.
+template <int NCB>
+__device__ __forceinline__ void scores(const Cols<NCB>& C, const bf16x8 (&ka)[4], const bf16x8 (&kb)[4], f32x4 (&s)[NCB][2]) {
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
     s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -131,6 +135,12 @@ __device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const 
       s[cb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[k], C.q[cb][k], s[cb][1], 0, 0, 0);
     }
   }
+}
+// The running maximum may lag behind by up to kLag octaves before accumulators are rescaled (weights up to 2^kLag lose nothing in
+// fp32), so a lane only has to look at its own rows; c2 > 0.
+constexpr float kLag = 8.f;
+template <int NCB, bool MASKED>
+__device__ __forceinline__ void soften(Cols<NCB>& C, f32x4 (&s)[NCB][2], bf16x8 (&ph)[NCB], bf16x8 (&pl)[NCB], int r0, int jg, float c2) {
   float mx[NCB];
   bool up = false;
 #pragma unroll
@@ -157,7 +167,6 @@ __device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const 
       for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
     }
   }
-  bf16x8 ph[NCB], pl[NCB];
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
     float p[8];
@@ -173,13 +182,14 @@ __device__ __forceinline__ void step(Cols<NCB>& C, const bf16x8 (&ka)[4], const 
     ph[cb] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
     pl[cb] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
   }
+}
+template <int NCB>
+__device__ __forceinline__ void add_rows(Cols<NCB>& C, int e, const bf16x8& vt, const bf16x8 (&ph)[NCB], const bf16x8 (&pl)[NCB]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-#pragma unroll
-    for (int cb = 0; cb < NCB; ++cb) {
-      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], ph[cb], C.acc[cb][e], 0, 0, 0);
-      C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], pl[cb], C.acc[cb][e], 0, 0, 0);
-    }
+  for (int cb = 0; cb < NCB; ++cb) {
+    C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[cb], C.acc[cb][e], 0, 0, 0);
+    C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[cb], C.acc[cb][e], 0, 0, 0);
+  }
 }
 template <int NCB>
 __device__ __forceinline__ void start(Cols<NCB>& C) {
@@ -200,23 +210,56 @@ __device__ __forceinline__ void load_query(bf16x8 (&q)[4], const uint16_t* row, 
   }
 }
 
-// Tiles [t0, t1) of 32 rows, wave w of the workgroup takes t0 + w, t0 + w + 4, ...; whole: no column masks anything in tiles below it.
-template <int NCB, bool PAGED>
-__device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1, int whole_from, int whole_to, int wave, int jg, int n, float c2, int& bad) {
+// Tiles [t0, t1) of 32 rows, wave w of NW takes t0 + w, t0 + w + NW, ...; no column masks anything from row whole_from to whole_to.  DEPTH tile
+// buffers; the rows of a later tile are requested into each half of a buffer as soon as its consumer is done with it.
+template <bool PAGED>
+struct Walker {
   Tile T;
+  Block A, B;
+  __device__ __forceinline__ void place(const Rows& R, int t, int& bad) {
+    A = block_of<PAGED>(R, t * kTile, bad);
+    B = block_of<PAGED>(R, t * kTile + 16, bad);
+  }
+};
+template <int NCB, int NW, int DEPTH, bool PAGED>
+__device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1, int whole_from, int whole_to, int wave, int jg, int n, float c2, int& bad) {
+  Walker<PAGED> W[DEPTH];
   int t = t0 + wave;
-  if (t < t1) issue<PAGED>(T, R, t * kTile, jg, n, bad);
-  for (; t < t1; t += kWaves) {
-    bf16x8 ka[4], kb[4], vt[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      ka[k] = __builtin_bit_cast(bf16x8, T.ka[k]);
-      kb[k] = __builtin_bit_cast(bf16x8, T.kb[k]);
+  for (int d = 0; d < DEPTH; ++d) {
+    const int td = t + d * NW;
+    if (td < t1) {
+      W[d].place(R, td, bad);
+      issue_k<PAGED>(W[d].T, R, W[d].A, W[d].B, td * kTile, jg, n);
+      issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, td * kTile, jg, n);
     }
-    turn_v(T.v, vt);
-    if (t + kWaves < t1) issue<PAGED>(T, R, (t + kWaves) * kTile, jg, n, bad);
-    if (t * kTile >= whole_from && (t + 1) * kTile <= whole_to) step<NCB, false>(C, ka, kb, vt, t * kTile, jg, c2);
-    else step<NCB, true>(C, ka, kb, vt, t * kTile, jg, c2);
+  }
+  for (; t < t1; t += DEPTH * NW) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int td = t + d * NW, next = td + DEPTH * NW, r0 = td * kTile;
+      if (td >= t1) break;
+      f32x4 s[NCB][2];
+      {
+        bf16x8 ka[4], kb[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          ka[k] = __builtin_bit_cast(bf16x8, W[d].T.ka[k]);
+          kb[k] = __builtin_bit_cast(bf16x8, W[d].T.kb[k]);
+        }
+        scores<NCB>(C, ka, kb, s);
+      }
+      if (next < t1) {
+        W[d].place(R, next, bad);
+        issue_k<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
+      }
+      bf16x8 ph[NCB], pl[NCB];
+      if (r0 >= whole_from && r0 + kTile <= whole_to) soften<NCB, false>(C, s, ph, pl, r0, jg, c2);
+      else soften<NCB, true>(C, s, ph, pl, r0, jg, c2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) add_rows<NCB>(C, e, turn_v(W[d].T.v, e), ph, pl);
+      if (next < t1) issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
+    }
   }
 }
 
@@ -358,7 +401,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
     Rows R = rows_of(a, a.lead, h);
     R.hi = seen.most - 1;
     const int tiles = (seen.most + kTile - 1) / kTile;
-    walk<NCB, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, seen.least, wave, jg, n, a.scale_log2, bad);
+    walk<NCB, kWaves, 2, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, seen.least, wave, jg, n, a.scale_log2, bad);
   }
   join<NCB, kWaves, true>(C, wave, 16 * NCB, 0, jg, n, lds, [&](int col) { return shared_record(a, col, h, split); });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
@@ -375,7 +418,7 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
   constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
   constexpr int kRowStep = kThreads / 16;
-  constexpr int kAhead = CG >= 8 ? 2 : 4 / kLoads;
+  constexpr int kAhead = CG >= 4 ? 2 : 1;
   static_assert(kLoads * kThreads == kRowsHere * 16 && kAhead >= 1, "whole rounds");
   constexpr int kStage = kRowsHere * 512;
   constexpr int kLds = 2 * kStage > 4 * join_floats<RG>(kCols) ? 2 * kStage : 4 * join_floats<RG>(kCols);
@@ -411,8 +454,8 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
           bad |= pc != page ? kGuardBlock : 0;
           at = (uint32_t)(pc * R.rpb + (row & ((1 << R.lg) - 1)));
         }
-        pk[slot][j] = load16(R.K + (uint64_t)at * R.k_st + piece * 16);
-        pv[slot][j] = load16(R.V + (uint64_t)at * R.v_st + piece * 16);
+        pk[slot][j] = load16<false>(R.K + (uint64_t)at * R.k_st + piece * 16);
+        pv[slot][j] = load16<false>(R.V + (uint64_t)at * R.v_st + piece * 16);
       }
     };
 #pragma unroll
@@ -448,8 +491,13 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
           const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * 256));
           vt[e] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
-        if (r0 + kTile <= seen.least) step<NCB, false>(C, ka, kb, vt, r0, jg, a.scale_log2);
-        else step<NCB, true>(C, ka, kb, vt, r0, jg, a.scale_log2);
+        f32x4 sc[NCB][2];
+        bf16x8 ph[NCB], pl[NCB];
+        scores<NCB>(C, ka, kb, sc);
+        if (r0 + kTile <= seen.least) soften<NCB, false>(C, sc, ph, pl, r0, jg, a.scale_log2);
+        else soften<NCB, true>(C, sc, ph, pl, r0, jg, a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) add_rows<NCB>(C, e, vt[e], ph, pl);
       }
     }
   }
@@ -458,15 +506,25 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
-// A sequence's own rows: a workgroup per KV head, split and sequence.
-template <bool PAGED>
-__global__ __launch_bounds__(kAttnThreads, 2) void own_rows_kernel(const SharedArgs a) {
-  __shared__ __align__(16) float lds[join_floats<kWaves>(16)];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
+// A sequence's own rows: n_own workgroups per KV head and sequence, and the merge.  The last of a pair's workgroups to finish merges the
+// records of all and those of the shared rows, which the launch before has left, into the output; records go from workgroup to workgroup at
+// device scope (stores and loads that name it, a count once the stores have been performed; the counter is zero between launches).
+// A pair with one workgroup keeps its record in LDS, and requests the shared rows' records before its waves are joined.
+constexpr int kOwnWaves = 4;
+constexpr int kOwnThreads = 64 * kOwnWaves;
+constexpr int kOwnAhead = 8;  // records a thread requests together
+constexpr int kDeviceScope = 16;  // cache-policy bit sc1 of the buffer instructions
+template <bool PAGED, bool ALONE>
+__global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedArgs a) {
+  __shared__ __align__(16) float lds[join_floats<kOwnWaves>(16)];
+  __shared__ __align__(16) float s_own[16][kPartStride];
+  __shared__ float s_w[16][kSlotCap];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, jg = lane >> 4, n = lane & 15;
   const int h = blockIdx.x, split = blockIdx.y, b = blockIdx.z;
+  const int64_t head0 = (int64_t)b * a.Hq + h * a.G;
   Cols<1> C;
   start(C);
-  load_query(C.q[0], a.q + ((int64_t)b * a.Hq + h * a.G + min(n, a.G - 1)) * kHeadDim, n < a.G, jg);
+  load_query(C.q[0], a.q + (head0 + min(n, a.G - 1)) * kHeadDim, n < a.G, jg);
   const int L = len_of(a, b), S = shared_of(a, b, L, len_of(a, a.lead));
   C.lo[0] = S;
   C.hi[0] = L;
@@ -476,12 +534,105 @@ __global__ __launch_bounds__(kAttnThreads, 2) void own_rows_kernel(const SharedA
     R.lo = S;
     R.hi = L - 1;
     const int first = S / kTile, tiles = (L + kTile - 1) / kTile - first;
-    walk<1, PAGED>(C, R, first + (int)((int64_t)tiles * split / a.n_own), first + (int)((int64_t)tiles * (split + 1) / a.n_own), S, L, wave, jg, n, a.scale_log2, bad);
+    walk<1, kOwnWaves, 1, PAGED>(C, R, first + (int)((int64_t)tiles * split / a.n_own), first + (int)((int64_t)tiles * (split + 1) / a.n_own), S, L, wave, jg, n,
+                                 a.scale_log2, bad);
   }
-  join<1, kWaves, true>(C, wave, 16, 0, jg, n, lds, [&](int col) -> float* {
-    return col < a.G ? a.part + (((int64_t)b * a.Hq + h * a.G + col) * kSlotCap + a.n_shared + split) * kPartStride : nullptr;
-  });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
+
+  // headers of a wave's heads, a record per lane; four output dims of every lanes-th record per thread, up to kRound heads at a time
+  constexpr int kRec = kPartStride * (int)sizeof(float), kHeads = 16 / kOwnWaves, kRound = kOwnThreads / (kHeadDim / 4);
+  const int n_rec = a.n_shared + (ALONE ? 0 : a.n_own);  // in memory
+  float* const pair = a.part + head0 * kSlotCap * kPartStride;
+  const __amdgpu_buffer_rsrc_t recs = __builtin_amdgcn_make_buffer_rsrc(pair, 0, a.G * kSlotCap * kRec, 0x00020000);
+  struct Share {
+    int quads, lanes, rl, item, g, c;
+  };
+  auto share_of = [&](int g0) {
+    Share r;
+    r.quads = min(kRound, a.G - g0) * (kHeadDim / 4);
+    r.lanes = kOwnThreads / r.quads;
+    r.rl = tid / r.quads;
+    r.item = tid % r.quads;
+    r.g = g0 + r.item / (kHeadDim / 4);
+    r.c = r.item % (kHeadDim / 4);
+    return r;
+  };
+  float2 hd[kHeads];
+  auto request_headers = [&]() {
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      const int g = wave + i * kOwnWaves;
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(recs, (min(g, a.G - 1) * kSlotCap + min(lane, max(n_rec - 1, 0))) * kRec, 0, ALONE ? 0 : kDeviceScope);
+      hd[i] = lane < n_rec ? make_float2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_float2(kNeg, 0.f);
+    }
+  };
+  f32x4 pre[kOwnAhead];
+  auto request = [&](const Share& r, int s0) {  // (records behind the last one repeat it)
+#pragma unroll
+    for (int i = 0; i < kOwnAhead; ++i) {
+      const int s = max(min(s0 + i * r.lanes, n_rec - 1), 0);
+      pre[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(recs, (min(r.g, a.G - 1) * kSlotCap + s) * kRec + 16 + 16 * r.c, 0,
+                                                                               ALONE ? 0 : kDeviceScope));
+    }
+  };
+  const Share first = share_of(0);
+  if (ALONE && n_rec > 0) {
+    request_headers();
+    request(first, first.rl);
+  }
+  join<1, kOwnWaves, true>(C, wave, 16, 0, jg, n, lds, [&](int col) { return s_own[col]; });
+  __syncthreads();
+  if (!ALONE) {
+    for (int i = tid; i < a.G * (kPartStride / 4); i += kOwnThreads) {
+      const int g = i / (kPartStride / 4), c4 = i % (kPartStride / 4);
+      __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(&s_own[g][4 * c4]), recs, (g * kSlotCap + a.n_shared + split) * kRec + 16 * c4, 0,
+                                             kDeviceScope);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's record stores have been performed
+    __shared__ uint32_t s_before;
+    __syncthreads();
+    uint32_t* const arrive = a.arrive + ((int64_t)b * a.Hkv + h) * kWaves * kArriveStride;
+    if (tid == 0) s_before = __hip_atomic_fetch_add(arrive, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s_before != (uint32_t)a.n_own - 1) return;
+    if (tid == 0) __hip_atomic_store(arrive, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    request_headers();
+    request(first, first.rl);
+  }
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int g = wave + i * kOwnWaves;
+    if (g >= a.G) break;
+    float2 ml = n_rec > 0 ? hd[i] : make_float2(kNeg, 0.f);
+    if (ALONE && lane == n_rec) ml = make_float2(s_own[g][0], s_own[g][1]);
+    const float w = __builtin_amdgcn_exp2f(ml.x - wave_max(ml.x));
+    const float Z = wave_sum_f(w * ml.y);
+    s_w[g][lane] = Z > 0.f ? w / Z : 0.f;
+  }
+  __syncthreads();
+  f32x4* s_o = reinterpret_cast<f32x4*>(lds);  // [lanes][quads]
+  for (int g0 = 0; g0 < a.G; g0 += kRound) {
+    const Share r = g0 == 0 ? first : share_of(g0);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (r.rl < r.lanes) {
+      for (int s0 = r.rl; s0 < n_rec; s0 += kOwnAhead * r.lanes) {
+        if (g0 > 0 || s0 > r.rl) request(r, s0);
+#pragma unroll
+        for (int i = 0; i < kOwnAhead; ++i) {
+          const int s = s0 + i * r.lanes;
+          if (s < n_rec) o += s_w[r.g][s] * pre[i];
+        }
+      }
+      if (ALONE && r.rl == 0) o += s_w[r.g][n_rec] * *reinterpret_cast<const f32x4*>(&s_own[r.g][4 + 4 * r.c]);
+      if (r.rl > 0) s_o[r.rl * r.quads + r.item] = o;
+    }
+    __syncthreads();
+    if (r.rl == 0) {
+      for (int k = 1; k < r.lanes; ++k) o += s_o[k * r.quads + r.item];
+      store_out4(a.out, (head0 + r.g) * kHeadDim + 4 * r.c, make_float4(o[0], o[1], o[2], o[3]), a.out_bf16 != 0);
+    }
+    __syncthreads();
+  }
 }
 
 }  // namespace
@@ -508,8 +659,13 @@ hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
 }
 hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s) {
   const dim3 grid(a.Hkv, a.n_own, a.B);
-  if (a.table != nullptr) hipLaunchKernelGGL(own_rows_kernel<true>, grid, dim3(kAttnThreads), 0, s, a);
-  else hipLaunchKernelGGL(own_rows_kernel<false>, grid, dim3(kAttnThreads), 0, s, a);
+  if (a.n_own == 1) {
+    if (a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, true>), grid, dim3(kOwnThreads), 0, s, a);
+    else hipLaunchKernelGGL((own_rows_kernel<false, true>), grid, dim3(kOwnThreads), 0, s, a);
+  } else {
+    if (a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, false>), grid, dim3(kOwnThreads), 0, s, a);
+    else hipLaunchKernelGGL((own_rows_kernel<false, false>), grid, dim3(kOwnThreads), 0, s, a);
+  }
   return hipGetLastError();
 }
 
