@@ -122,74 +122,84 @@ struct Cols {
   float m[NCB], l[NCB];  // l: of this lane's rows
   int lo[NCB], hi[NCB];  // rows this column sees
 };
-// One tile in three parts: products with K, weights, products with V.  Each does all blocks of columns, with one branch in
-// all, so that matrix and vector instructions of different blocks overlap.
+// The parts of a tile.  Products with K:
 template <int NCB>
 __device__ __forceinline__ void scores(const Cols<NCB>& C, const bf16x8 (&ka)[4], const bf16x8 (&kb)[4], f32x4 (&s)[NCB][2]) {
 #pragma unroll
-  for (int cb = 0; cb < NCB; ++cb) {
-    s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int cb = 0; cb < NCB; ++cb) s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int cb = 0; cb < NCB; ++cb) {
       s[cb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[k], C.q[cb][k], s[cb][0], 0, 0, 0);
       s[cb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[k], C.q[cb][k], s[cb][1], 0, 0, 0);
     }
-  }
 }
-// The running maximum may lag behind by up to kLag octaves before accumulators are rescaled (weights up to 2^kLag lose nothing in
-// fp32), so a lane only has to look at its own rows; c2 > 0.
-constexpr float kLag = 8.f;
-template <int NCB, bool MASKED>
-__device__ __forceinline__ void soften(Cols<NCB>& C, f32x4 (&s)[NCB][2], bf16x8 (&ph)[NCB], bf16x8 (&pl)[NCB], int r0, int jg, float c2) {
-  float mx[NCB];
+// What a column does not see.
+template <int NCB>
+__device__ __forceinline__ void mask(const Cols<NCB>& C, f32x4 (&s)[NCB][2], int r0, int jg) {
+#pragma unroll
+  for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 16 * (i >> 2) + 4 * jg + (i & 3);
+      s[cb][i >> 2][i & 3] = r >= C.lo[cb] && r < C.hi[cb] ? s[cb][i >> 2][i & 3] : -__builtin_inff();
+    }
+}
+// The weights of a block of columns as two bf16 terms, and their sum over the lane's rows.
+struct Weights {
+  bf16x8 hi, lo;
+};
+__device__ __forceinline__ float weights_of(const f32x4 (&s)[2], float m, float c2, Weights& w) {
+  float p[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -m));  // a masked row: 2^-inf = 0
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    hi[i] = round2(p[2 * i], p[2 * i + 1]);
+    lo[i] = round2(p[2 * i] - __uint_as_float(hi[i] << 16), p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
+  }
+  w.hi = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+  w.lo = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+// All blocks' weights.  The running maximum may lag behind the rows: only when a lane's weights add up to more than kLag (they are then far
+// from what fp32 or bf16 lose anything at) is it brought up, accumulators and sums rescaled and the weights made again.  That
+// happens in the first tile, whose maximum is kNeg, and rarely later; the common way looks for no maximum at all.  c2 > 0.
+constexpr float kLag = 256.f;
+template <int NCB>
+__device__ __forceinline__ void soften(Cols<NCB>& C, const f32x4 (&s)[NCB][2], Weights (&w)[NCB], float c2) {
+  float sum[NCB];
   bool up = false;
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
-    if (MASKED) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = r0 + 16 * (i >> 2) + 4 * jg + (i & 3);
-        s[cb][i >> 2][i & 3] = r >= C.lo[cb] && r < C.hi[cb] ? s[cb][i >> 2][i & 3] : -__builtin_inff();
-      }
-    }
-    mx[cb] = fmaxf(fmaxf(fmaxf(s[cb][0][0], s[cb][0][1]), fmaxf(s[cb][0][2], s[cb][0][3])),
-                   fmaxf(fmaxf(s[cb][1][0], s[cb][1][1]), fmaxf(s[cb][1][2], s[cb][1][3]))) * c2;
-    up |= mx[cb] > C.m[cb] + kLag;
+    sum[cb] = weights_of(s[cb], C.m[cb], c2, w[cb]);
+    up |= sum[cb] > kLag;
   }
-  if (__any(up)) {
+  if (__builtin_expect(__any(up), 0)) {
 #pragma unroll
     for (int cb = 0; cb < NCB; ++cb) {
-      const float m1 = fmaxf(across_max(mx[cb]), C.m[cb]);  // (not below kNeg: finite)
+      const float mx = fmaxf(fmaxf(fmaxf(s[cb][0][0], s[cb][0][1]), fmaxf(s[cb][0][2], s[cb][0][3])),
+                             fmaxf(fmaxf(s[cb][1][0], s[cb][1][1]), fmaxf(s[cb][1][2], s[cb][1][3]))) * c2;
+      const float m1 = fmaxf(across_max(mx), C.m[cb]);  // (not below kNeg: finite)
       const float f = __builtin_amdgcn_exp2f(C.m[cb] - m1);
       C.m[cb] = m1;
       C.l[cb] *= f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
+      sum[cb] = weights_of(s[cb], m1, c2, w[cb]);
     }
   }
 #pragma unroll
-  for (int cb = 0; cb < NCB; ++cb) {
-    float p[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[cb][i >> 2][i & 3], c2, -C.m[cb]));  // a masked row: 2^-inf = 0
-    C.l[cb] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      hi[i] = round2(p[2 * i], p[2 * i + 1]);
-      lo[i] = round2(p[2 * i] - __uint_as_float(hi[i] << 16), p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
-    }
-    ph[cb] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    pl[cb] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-  }
+  for (int cb = 0; cb < NCB; ++cb) C.l[cb] += sum[cb];
 }
-template <int NCB>
-__device__ __forceinline__ void add_rows(Cols<NCB>& C, int e, const bf16x8& vt, const bf16x8 (&ph)[NCB], const bf16x8 (&pl)[NCB]) {
+// Products with V.
+__device__ __forceinline__ void add_rows(f32x4 (&acc)[8], const bf16x8 (&vt)[8], const Weights& w) {
 #pragma unroll
-  for (int cb = 0; cb < NCB; ++cb) {
-    C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph[cb], C.acc[cb][e], 0, 0, 0);
-    C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl[cb], C.acc[cb][e], 0, 0, 0);
-  }
+  for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.hi, acc[e], 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.lo, acc[e], 0, 0, 0);
 }
 template <int NCB>
 __device__ __forceinline__ void start(Cols<NCB>& C) {
@@ -253,11 +263,18 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
         W[d].place(R, next, bad);
         issue_k<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
       }
-      bf16x8 ph[NCB], pl[NCB];
-      if (r0 >= whole_from && r0 + kTile <= whole_to) soften<NCB, false>(C, s, ph, pl, r0, jg, c2);
-      else soften<NCB, true>(C, s, ph, pl, r0, jg, c2);
+      if (r0 < whole_from || r0 + kTile > whole_to) mask<NCB>(C, s, r0, jg);
+      Weights w[NCB];
+      soften<NCB>(C, s, w, c2);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) add_rows<NCB>(C, e, turn_v(W[d].T.v, e), ph, pl);
+      for (int e = 0; e < 8; ++e) {
+        const bf16x8 vt = turn_v(W[d].T.v, e);
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) {
+          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].hi, C.acc[cb][e], 0, 0, 0);
+          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].lo, C.acc[cb][e], 0, 0, 0);
+        }
+      }
       if (next < t1) issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
     }
   }
@@ -391,7 +408,7 @@ __device__ __forceinline__ float* shared_record(const SharedArgs& a, int c, int 
 template <int NCB, bool PAGED>
 __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const SharedArgs a) {
   __shared__ __align__(16) float lds[join_floats<kWaves>(16 * NCB)];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
   const int h = blockIdx.x, split = blockIdx.y;
   Cols<NCB> C;
   start(C);
@@ -407,23 +424,33 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
+// A barrier that no instruction is scheduled across.
+__device__ __forceinline__ void change_turns() {
+  __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // The shared rows for many columns: the tiles go through LDS, where all waves of the workgroup read them.  CG groups of 16 NCB columns,
-// and RG groups of waves that take a tile each of a stage of RG tiles.  Every thread requests kAhead stages in front (64 KB a compute unit
-// on their way), as 16 bytes of a row each, and stores a stage into one of two buffers while the other is read: one barrier per stage.
-// In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read together,
-// one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of four rows),
-// lies in different banks.
+// and RG groups of waves that take a tile each of a stage of RG tiles.
+// - Every thread requests kAhead stages in front, as 16 bytes of a row each, and stores a stage into one of kRing buffers: one barrier per stage (two
+//   with two buffers).  In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read
+//   together, one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of
+//   four rows), lies in different banks.
+// - A stage's products with K are made while the stage before is turned into weights: matrix and vector instructions of one wave that do
+//   not depend on each other, side by side, so that neither pipe waits for the other.
 template <int NCB, int CG, int RG, bool PAGED>
 __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
   constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
   constexpr int kRowStep = kThreads / 16;
-  constexpr int kAhead = CG >= 4 ? 2 : 1;
-  static_assert(kLoads * kThreads == kRowsHere * 16 && kAhead >= 1, "whole rounds");
-  constexpr int kStage = kRowsHere * 512;
-  constexpr int kLds = 2 * kStage > 4 * join_floats<RG>(kCols) ? 2 * kStage : 4 * join_floats<RG>(kCols);
+  constexpr int kAhead = 2;
+  static_assert(kLoads * kThreads == kRowsHere * 16, "whole rounds");
+  static_assert(kThreads == 512 && RG <= 2, "eight waves, two on each SIMD");
+  constexpr int kStage = kRowsHere * 512, kRing = 3;
+  constexpr int kLds = kRing * kStage > 4 * join_floats<RG>(kCols) ? kRing * kStage : 4 * join_floats<RG>(kCols);
   __shared__ __align__(16) unsigned char lds[kLds];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, jg = lane >> 4, n = lane & 15;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, jg = lane >> 4, n = lane & 15;
   const int cg = wave % CG, rg = wave / CG;
   const int h = blockIdx.x, split = blockIdx.y, c_first = blockIdx.z * kCols, c0 = 16 * NCB * cg;
   __shared__ int s_most[CG * RG];
@@ -436,70 +463,99 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
 #pragma unroll
   for (int w = 0; w < CG; ++w) most = max(most, s_most[w]);
   most = __builtin_amdgcn_readfirstlane(most);
+  const float c2 = a.scale_log2;
   int bad = 0;
-  if (most > 0) {
+  const int stages = (most + kRowsHere - 1) / kRowsHere;
+  const int t0 = (int)((int64_t)stages * split / a.n_shared), t1 = (int)((int64_t)stages * (split + 1) / a.n_shared);
+  if (t0 < t1) {
     const Rows R = rows_of(a, a.lead, h);
     const int last = most - 1;
-    const int stages = (most + kRowsHere - 1) / kRowsHere;
-    const int t0 = (int)((int64_t)stages * split / a.n_shared), t1 = (int)((int64_t)stages * (split + 1) / a.n_shared);
     const int my_row = tid >> 4, piece = tid & 15;
     uint4 pk[kAhead][kLoads], pv[kAhead][kLoads];
     auto request = [&](int slot, int t) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int row = min(t * kRowsHere + my_row + j * kRowStep, last);
-        uint32_t at = (uint32_t)row;
         if (PAGED) {
           const int page = R.table[row >> R.lg], pc = min(max(page, 0), R.n_blocks - 1);
           bad |= pc != page ? kGuardBlock : 0;
-          at = (uint32_t)(pc * R.rpb + (row & ((1 << R.lg) - 1)));
+          const uint32_t at = (uint32_t)(pc * R.rpb + (row & ((1 << R.lg) - 1)));
+          pk[slot][j] = load16<false>(R.K + (uint64_t)at * R.k_st + piece * 16);
+          pv[slot][j] = load16<false>(R.V + (uint64_t)at * R.v_st + piece * 16);
+        } else {  // a KV head's rows lie within 4 GiB
+          pk[slot][j] = load16<false>(R.K + ((uint32_t)row * (uint32_t)R.k_st + piece * 16));
+          pv[slot][j] = load16<false>(R.V + ((uint32_t)row * (uint32_t)R.v_st + piece * 16));
         }
-        pk[slot][j] = load16<false>(R.K + (uint64_t)at * R.k_st + piece * 16);
-        pv[slot][j] = load16<false>(R.V + (uint64_t)at * R.v_st + piece * 16);
       }
     };
+    auto stash = [&](int slot, int buf) {
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-      if (t0 + s < t1) request(s, t0 + s);
+      for (int j = 0; j < kLoads; ++j) {
+        const int r = my_row + j * kRowStep;
+        *reinterpret_cast<uint4*>(lds + buf + r * 256 + ((piece ^ (r & 15)) << 4)) = pk[slot][j];
+        *reinterpret_cast<uint4*>(lds + buf + kRowsHere * 256 + r * 256 + (((piece >> 1) ^ (r & 7)) << 5) + ((piece & 1) << 4)) = pv[slot][j];
+      }
+    };
     const unsigned char* k_at = lds + (rg * kTile + n) * 256;
     const unsigned char* v_at = lds + kRowsHere * 256 + (rg * kTile + 4 * jg + (n >> 2)) * 256 + 8 * (n & 3);
     const int v_turn = (4 * jg + (n >> 2)) & 7;
-    for (int t = t0; t < t1; t += kAhead) {
+    auto read_k = [&](int buf, bf16x8 (&ka)[4], bf16x8 (&kb)[4]) {
 #pragma unroll
-      for (int s = 0; s < kAhead; ++s) {
-        if (t + s >= t1) break;
-        const int buf = ((t + s - t0) & 1) * kStage;
+      for (int k = 0; k < 4; ++k) {
+        ka[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + (((4 * k + jg) ^ n) << 4));
+        kb[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + 16 * 256 + (((4 * k + jg) ^ n) << 4));
+      }
+    };
+    auto read_v = [&](int buf, bf16x8 (&vt)[8]) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const int r = my_row + j * kRowStep;
-          *reinterpret_cast<uint4*>(lds + buf + r * 256 + ((piece ^ (r & 15)) << 4)) = pk[s][j];
-          *reinterpret_cast<uint4*>(lds + buf + kRowsHere * 256 + r * 256 + (((piece >> 1) ^ (r & 7)) << 5) + ((piece & 1) << 4)) = pv[s][j];
-        }
-        if (t + s + kAhead < t1) request(s, t + s + kAhead);
-        __syncthreads();
-        const int r0 = (t + s) * kRowsHere + rg * kTile;
-        bf16x8 ka[4], kb[4], vt[8];
+      for (int e = 0; e < 8; ++e) {
+        const unsigned char* p = v_at + buf + ((e ^ v_turn) << 5);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * 256));
+        vt[e] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    };
+    // Waves w and w + 4 share a SIMD.  They take turns: one makes a stage's products while the other turns its logits into weights and reads operands.
+    const int turn = wave >> 2;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          ka[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + (((4 * k + jg) ^ n) << 4));
-          kb[k] = *reinterpret_cast<const bf16x8*>(k_at + buf + 16 * 256 + (((4 * k + jg) ^ n) << 4));
-        }
+    for (int s = 0; s < kAhead; ++s) request(s, min(t0 + s, t1 - 1));
+    int slot = 0, put = 0;
+    auto pass_on = [&](int from, int t) {  // stage t from registers into its buffer; the one kAhead further on requested
+      stash(from, put);
+      request(from, min(t + kAhead, t1 - 1));
+      put = put + kStage == kRing * kStage ? 0 : put + kStage;
+    };
+    pass_on(0, t0);
+    pass_on(1 % kAhead, t0 + 1);
+    __syncthreads();
+    f32x4 s[NCB][2];
+    bf16x8 ka[4], kb[4], vt[8];
+    read_k(0, ka, kb);
+    scores<NCB>(C, ka, kb, s);
+    if (turn == 1) __syncthreads();
+    for (int tt = t0; tt < t1; tt += kAhead) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const unsigned char* p = v_at + buf + ((e ^ v_turn) << 5);
-          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * 256));
-          vt[e] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-        f32x4 sc[NCB][2];
-        bf16x8 ph[NCB], pl[NCB];
-        scores<NCB>(C, ka, kb, sc);
-        if (r0 + kTile <= seen.least) soften<NCB, false>(C, sc, ph, pl, r0, jg, a.scale_log2);
-        else soften<NCB, true>(C, sc, ph, pl, r0, jg, a.scale_log2);
+      for (int u = 0; u < kAhead; ++u) {
+        // stage t: logits to weights; operands of its products with V and of stage t + 1's with K (behind the last stage: of what lies there, not used)
+        const int t = tt + u;
+        if (t >= t1) break;
+        const int next = slot + kStage == kRing * kStage ? 0 : slot + kStage;
+        const int r0 = t * kRowsHere + rg * kTile;
+        pass_on((u + 2) % kAhead, t + 2);
+        read_v(slot, vt);
+        if (r0 + kTile > seen.least) mask<NCB>(C, s, r0, jg);
+        Weights w[NCB];
+        soften<NCB>(C, s, w, c2);
+        change_turns();
+        read_k(next, ka, kb);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) add_rows<NCB>(C, e, vt[e], ph, pl);
+        for (int cb = 0; cb < NCB; ++cb) add_rows(C.acc[cb], vt, w[cb]);
+        scores<NCB>(C, ka, kb, s);
+        change_turns();
+        slot = next;
       }
     }
+    if (turn == 0) __syncthreads();
   }
   if (RG > 1) __syncthreads();  // the buffers are read no more
   join<NCB, RG, false>(C, rg, kCols, c0, jg, n, reinterpret_cast<float*>(lds), [&](int col) { return shared_record(a, c_first + col, h, split); });
@@ -519,7 +575,7 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
   __shared__ __align__(16) float lds[join_floats<kOwnWaves>(16)];
   __shared__ __align__(16) float s_own[16][kPartStride];
   __shared__ float s_w[16][kSlotCap];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, jg = lane >> 4, n = lane & 15;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, jg = lane >> 4, n = lane & 15;
   const int h = blockIdx.x, split = blockIdx.y, b = blockIdx.z;
   const int64_t head0 = (int64_t)b * a.Hq + h * a.G;
   Cols<1> C;
@@ -651,7 +707,7 @@ hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
   switch (cols) {
     case 16: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 1); break;
     case 32: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 2); break;
-    case 64: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 2, 4); break;
+    case 64: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2); break;
     case 128: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2); break;
     default: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1);
   }
