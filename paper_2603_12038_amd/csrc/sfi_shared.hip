@@ -424,31 +424,27 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
-// A barrier that no instruction is scheduled across.
-__device__ __forceinline__ void change_turns() {
-  __builtin_amdgcn_sched_barrier(0);
-  __syncthreads();
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 // The shared rows for many columns: the tiles go through LDS, where all waves of the workgroup read them.  CG groups of 16 NCB columns,
 // and RG groups of waves that take a tile each of a stage of RG tiles.
-// - Every thread requests kAhead stages in front, as 16 bytes of a row each, and stores a stage into one of kRing buffers: one barrier per stage (two
-//   with two buffers).  In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read
+// - Every thread requests kAhead stages in front, as 16 bytes of a row each, and stores a stage into one of two buffers: one barrier per
+//   stage.  In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read
 //   together, one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of
 //   four rows), lies in different banks.
-// - A stage's products with K are made while the stage before is turned into weights: matrix and vector instructions of one wave that do
-//   not depend on each other, side by side, so that neither pipe waits for the other.
+// - Eight waves, two on each SIMD.  64 sequences of 64 heads over 32768 rows: 105 to 110 us, 69.3 GFLOP and half as many again for the weights' second terms,
+//   950 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200; the matrix pipe is busy 46 % of the time, the vector
+//   pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's products with V beside stage t + 1's
+//   weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.  32 sequences of 32
+//   heads over 16384 rows, paged (128 columns): 29 us for 134 MB, 4.7 TB/s, and 17 MB of records.
 template <int NCB, int CG, int RG, bool PAGED>
 __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
   constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
   constexpr int kRowStep = kThreads / 16;
-  constexpr int kAhead = 2;
+  constexpr int kAhead = 2;  // stages on their way, and buffers
   static_assert(kLoads * kThreads == kRowsHere * 16, "whole rounds");
   static_assert(kThreads == 512 && RG <= 2, "eight waves, two on each SIMD");
-  constexpr int kStage = kRowsHere * 512, kRing = 3;
-  constexpr int kLds = kRing * kStage > 4 * join_floats<RG>(kCols) ? kRing * kStage : 4 * join_floats<RG>(kCols);
+  constexpr int kStage = kRowsHere * 512;
+  constexpr int kLds = 2 * kStage > 4 * join_floats<RG>(kCols) ? 2 * kStage : 4 * join_floats<RG>(kCols);
   __shared__ __align__(16) unsigned char lds[kLds];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, jg = lane >> 4, n = lane & 15;
   const int cg = wave % CG, rg = wave / CG;
@@ -515,47 +511,29 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
         vt[e] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
       }
     };
-    // Waves w and w + 4 share a SIMD.  They take turns: one makes a stage's products while the other turns its logits into weights and reads operands.
-    const int turn = wave >> 2;
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) request(s, min(t0 + s, t1 - 1));
-    int slot = 0, put = 0;
-    auto pass_on = [&](int from, int t) {  // stage t from registers into its buffer; the one kAhead further on requested
-      stash(from, put);
-      request(from, min(t + kAhead, t1 - 1));
-      put = put + kStage == kRing * kStage ? 0 : put + kStage;
-    };
-    pass_on(0, t0);
-    pass_on(1 % kAhead, t0 + 1);
-    __syncthreads();
     f32x4 s[NCB][2];
     bf16x8 ka[4], kb[4], vt[8];
-    read_k(0, ka, kb);
-    scores<NCB>(C, ka, kb, s);
-    if (turn == 1) __syncthreads();
+    Weights w[NCB];
     for (int tt = t0; tt < t1; tt += kAhead) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        // stage t: logits to weights; operands of its products with V and of stage t + 1's with K (behind the last stage: of what lies there, not used)
         const int t = tt + u;
         if (t >= t1) break;
-        const int next = slot + kStage == kRing * kStage ? 0 : slot + kStage;
-        const int r0 = t * kRowsHere + rg * kTile;
-        pass_on((u + 2) % kAhead, t + 2);
-        read_v(slot, vt);
+        const int r0 = t * kRowsHere + rg * kTile, buf = u * kStage;
+        stash(u, buf);
+        request(u, min(t + kAhead, t1 - 1));
+        __syncthreads();
+        read_k(buf, ka, kb);
+        read_v(buf, vt);
+        scores<NCB>(C, ka, kb, s);
         if (r0 + kTile > seen.least) mask<NCB>(C, s, r0, jg);
-        Weights w[NCB];
         soften<NCB>(C, s, w, c2);
-        change_turns();
-        read_k(next, ka, kb);
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb) add_rows(C.acc[cb], vt, w[cb]);
-        scores<NCB>(C, ka, kb, s);
-        change_turns();
-        slot = next;
       }
     }
-    if (turn == 0) __syncthreads();
   }
   if (RG > 1) __syncthreads();  // the buffers are read no more
   join<NCB, RG, false>(C, rg, kCols, c0, jg, n, reinterpret_cast<float*>(lds), [&](int col) { return shared_record(a, c_first + col, h, split); });
