@@ -353,11 +353,11 @@ def sfi_set_rope(ctx, rot_dim: int, base: float = 10000.0, interleaved: bool = F
 def sfi_rope_append(ctx, q, k, v, ctx_len, n_new, pos, q_out, K, V, stream=None) -> None:
     """q: bf16 tensor [B, new, Hq, 128], k, v: [B, new, Hkv, 128], the heads of a row contiguous (views of one projection's output will do);
     q and q_out (contiguous) may be None together.  n_new, pos: int32 [B] or None."""
-    for t in (q, k, v):
-        assert t is None or (t.dim() == 4 and t.shape[1] == k.shape[1] and t.stride(3) == 1 and (t.shape[2] == 1 or t.stride(2) == t.shape[3]))
-    assert q_out is None or q_out.is_contiguous()
-    (_hot or _load_hot()).sfi_rope_append(ctx, q, 0 if q is None else q.stride(0), 0 if q is None else q.stride(1), k, k.stride(0), k.stride(1),
-                                          v, v.stride(0), v.stride(1), ctx_len, n_new, pos, k.shape[1], q_out, K, V, stream)
+    qs, ks, vs = (0, 0, 128, 1) if q is None else q.stride(), k.stride(), v.stride()
+    _, new, heads, d = k.shape
+    assert qs[3] == ks[3] == vs[3] == 1 and (heads == 1 or ks[2] == vs[2] == d) and (qs[2] == d or q.shape[2] == 1) and v.shape == k.shape
+    assert q is None or (q.shape[1] == new and q_out.is_contiguous())
+    (_hot or _load_hot()).sfi_rope_append(ctx, q, qs[0], qs[1], k, ks[0], ks[1], v, vs[0], vs[1], ctx_len, n_new, pos, new, q_out, K, V, stream)
 
 
 def sfi_shared_attn(ctx, q, K, V, ctx_len, shared_len, lead: int, max_shared: int, max_len: int, out, stream=None) -> None:

@@ -734,7 +734,7 @@ namespace {
 // J-only softmax statistics) left in the workspace.
 int slow_attn_impl(sfi_ctx* x, const void* q, const void* K, const void* V, const int32_t* ctx_len, int ml,
                    float* out, hipStream_t st, bool merge_later = false, const int32_t* q_len = nullptr, bool select_next = false,
-                   bool rounded = false) {
+                   bool three_terms = false) {
   AttnArgs a;
   fill_attn(x, &a, q, K, V, ctx_len);
   a.q_len = q_len;
@@ -756,7 +756,7 @@ int slow_attn_impl(sfi_ctx* x, const void* q, const void* K, const void* V, cons
   x->last_dense_scored = select_next && score_in_dense(x, a, ml);
   if (x->last_dense_scored && set_dense_scores(x, &a, st) != SFI_OK) return SFI_ELAUNCH;
   x->last_dense_splits = a.n_split;
-  { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_attn_dense(a, x->cfg.batch, a.n_split, st, rounded)); if (!t.stop()) return SFI_ELAUNCH; }
+  { StageTimer t(x, st, SFI_STAGE_ATTN); SFI_TRY(launch_attn_dense(a, x->cfg.batch, a.n_split, st, three_terms)); if (!t.stop()) return SFI_ELAUNCH; }
   if (merge_later) return SFI_OK;  // the Selector's scoring launch merges
   MergeArgs m{x->ws.part, out, nullptr, x->cfg.n_q_heads, a.n_split, 0, 0, x->ws.jstat, a.plan_batch > 0 ? x->ws.seq_rec : nullptr, x->G, x->alpha, x->cfg.out_bf16};
   { StageTimer t(x, st, SFI_STAGE_MERGE); SFI_TRY(launch_merge(m, x->cfg.batch, st)); if (!t.stop()) return SFI_ELAUNCH; }

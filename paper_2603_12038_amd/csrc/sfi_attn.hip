@@ -417,16 +417,16 @@ __device__ __forceinline__ void mask_tail(Tile& T, float (&y)[8], int jg, int p0
 // which is rare after the first tiles) and the weights as two bf16 terms, hi + lo ~ 16 bits.
 // Masked rows carry y = kNeg; every tile handed in has at least one unmasked row, so each head's
 // maximum is finite and 2^(kNeg - max) is exactly 0.
-// ROUND: both terms to nearest even, not cut off: the weights' loss is below 2^-17 and has no direction (cut off, a sum over few
-// rows of like weight is 6e-6 too small).
+// THREE (sfi_weight_attn): three terms, each to nearest even: all of the weight's 24 bits.  (Cut off at 16 bits, weights of few rows are all 6e-6 too small.)
+// The third takes 8 of 32 products a tile, and the launch's time is the rows it reads.
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 __device__ __forceinline__ uint32_t round2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
-template <bool ROUND = false>
+template <bool THREE = false>
 __device__ __forceinline__ void softmax_phase(const float (&y)[8], f32x4 (&acc)[8], float& m_run, float& l_run, int jg,
-                                              bf16x8& a_hi, bf16x8& a_lo) {
+                                              bf16x8& a_hi, bf16x8& a_lo, bf16x8* a_rest = nullptr) {
   float mt = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
   const float m_new = fmaxf(m_run, rows_max(mt));
   if (__ballot(m_new > m_run) != 0ull) {
@@ -442,18 +442,21 @@ __device__ __forceinline__ void softmax_phase(const float (&y)[8], f32x4 (&acc)[
     m_run = m_new;
   }
   float pr[8], lo[8], ps = 0.f;
-  if (ROUND) {
-    uint32_t hi[4], rest[4];
+  if (THREE) {
+    uint32_t hi[4], mid[4], rest[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float p0 = fast_exp2(y[2 * i] - m_run), p1 = fast_exp2(y[2 * i + 1] - m_run);
       ps += p0 + p1;
       hi[i] = round2(p0, p1);
-      rest[i] = round2(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
+      const float r0 = p0 - __uint_as_float(hi[i] << 16), r1 = p1 - __uint_as_float(hi[i] & 0xffff0000u);
+      mid[i] = round2(r0, r1);
+      rest[i] = round2(r0 - __uint_as_float(mid[i] << 16), r1 - __uint_as_float(mid[i] & 0xffff0000u));
     }
     l_run += ps;
     a_hi = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    a_lo = as_bf16x8(make_uint4(rest[0], rest[1], rest[2], rest[3]));
+    a_lo = as_bf16x8(make_uint4(mid[0], mid[1], mid[2], mid[3]));
+    *a_rest = as_bf16x8(make_uint4(rest[0], rest[1], rest[2], rest[3]));
     return;
   }
 #pragma unroll
@@ -470,7 +473,8 @@ __device__ __forceinline__ void softmax_phase(const float (&y)[8], f32x4 (&acc)[
 }
 
 // Phase 3: O += P V, one product per dim offset e: element e of each of the 8 rows this lane holds.
-__device__ __forceinline__ void pv_phase(const Tile& T, const bf16x8& a_hi, const bf16x8& a_lo, f32x4 (&acc)[8]) {
+template <bool THREE = false>
+__device__ __forceinline__ void pv_phase(const Tile& T, const bf16x8& a_hi, const bf16x8& a_lo, f32x4 (&acc)[8], const bf16x8* a_rest = nullptr) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     uint32_t c[8];
@@ -482,6 +486,7 @@ __device__ __forceinline__ void pv_phase(const Tile& T, const bf16x8& a_hi, cons
     const bf16x8 b_e = as_bf16x8(bv);
     acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a_hi, b_e, acc[e], 0, 0, 0);
     acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a_lo, b_e, acc[e], 0, 0, 0);
+    if (THREE) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*a_rest, b_e, acc[e], 0, 0, 0);
   }
 }
 
@@ -800,7 +805,7 @@ struct ListWalk {
 // dense kernel
 // ------------------------------------------------------------------------------------------------
 // PAGED: K / V are block pools addressed through the sequence's block table.
-// EXPOSE 1: also write y over J for the Selector; -1: the same, with softmax_phase's ROUND (sfi_weight_attn); 2: y and the squared key norms; 3, 4: y (and the norms) stay in LDS as far as they fit, for score_tail.
+// EXPOSE 1: also write y over J for the Selector; -1: the same, with softmax_phase's THREE (sfi_weight_attn); 2: y and the squared key norms; 3, 4: y (and the norms) stay in LDS as far as they fit, for score_tail.
 // BIG: twice the logits stash per wave, which leaves room for one workgroup per compute unit only
 // (launches where every sequence is dense, and the planned launch, run one per unit anyway; the ragged
 // step's launch with a workgroup per cell keeps two, although that kernel spills 6 to 26 of its 256 registers: with one,
@@ -1041,9 +1046,9 @@ __device__ __forceinline__ void dense_body(const AttnArgs& a, const DenseShare& 
     const int p0 = (inJ ? t : t - nTJ) * kTile;
     const int N = inJ ? NJ : NS;
     if (p0 + kTile > N) mask_tail<WIDE>(T, y, jg, p0, N);
-    bf16x8 a_hi, a_lo;
-    softmax_phase<EXPOSE == -1>(y, acc, m_run, l_run, jg, a_hi, a_lo);
-    pv_phase(T, a_hi, a_lo, acc);
+    bf16x8 a_hi, a_lo, a_rest;
+    softmax_phase<EXPOSE == -1>(y, acc, m_run, l_run, jg, a_hi, a_lo, &a_rest);
+    pv_phase<EXPOSE == -1>(T, a_hi, a_lo, acc, &a_rest);
     if (!kRefill) return;
     if (PAGED) issue_v_rows<uint64_t>(T, R, pra, prb);
     else issue_v_tile(T, t + NB * step);
@@ -2701,7 +2706,7 @@ hipError_t launch_trigger(const int32_t* last_token, const uint32_t* bitmap, int
 }
 
 template <bool PAGED>
-static void launch_dense_t(const AttnArgs& a, dim3 grid, bool rounded, hipStream_t s) {
+static void launch_dense_t(const AttnArgs& a, dim3 grid, bool three_terms, hipStream_t s) {
   if (a.plan_batch > 0) {
     const dim3 pgrid(a.Hkv, std::max(a.plan_wgs, a.plan_even * a.plan_batch));
     const uint32_t strides = (uint32_t)a.ms | (uint32_t)a.fs << 16;
@@ -2710,14 +2715,14 @@ static void launch_dense_t(const AttnArgs& a, dim3 grid, bool rounded, hipStream
                      a.q_len, strides, a.plan_batch, a.plan_wgs, 1.0f / (float)a.plan_min, a.n_sink, a.recent, a.len_cap, a)
     if (a.logits == nullptr) SFI_PLANNED(0);
     else if (a.with_knorm && a.met != nullptr) SFI_PLANNED(4);
-    else if (rounded) SFI_PLANNED(-1);
+    else if (three_terms) SFI_PLANNED(-1);
     else if (a.with_knorm) SFI_PLANNED(2);
     else if (a.met != nullptr) SFI_PLANNED(3);
     else SFI_PLANNED(1);
 #undef SFI_PLANNED
     return;
   }
-  if (rounded) {
+  if (three_terms) {
     hipLaunchKernelGGL((attn_dense_kernel<-1, PAGED, true>), grid, dim3(kAttnThreads), 0, s, a);
     return;
   }
@@ -2751,10 +2756,10 @@ static void launch_dense_t(const AttnArgs& a, dim3 grid, bool rounded, hipStream
     hipLaunchKernelGGL((attn_dense_kernel<0, PAGED>), grid, dim3(kAttnThreads), 0, s, a);
   }
 }
-hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool rounded) {
+hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool three_terms) {
   const dim3 grid(a.Hkv, n_slots, B);
-  if (a.table != nullptr) launch_dense_t<true>(a, grid, rounded, s);
-  else launch_dense_t<false>(a, grid, rounded, s);
+  if (a.table != nullptr) launch_dense_t<true>(a, grid, three_terms, s);
+  else launch_dense_t<false>(a, grid, three_terms, s);
   return hipGetLastError();
 }
 hipError_t launch_attn_ragged(const AttnArgs& d, const AttnArgs& f, bool balanced, hipStream_t s) {

@@ -354,8 +354,8 @@ struct SelArgs {
   int32_t n_place;         //   ... how many of them it has
 };
 
-// rounded: logits exposed (no key norms), the weights' two terms to nearest
-hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool rounded = false);
+// three_terms: logits exposed (no key norms), the weights in three terms
+hipError_t launch_attn_dense(const AttnArgs& a, int B, int n_slots, hipStream_t s, bool three_terms = false);
 hipError_t launch_attn_evidence(const AttnArgs& a, int B, int n_slots, hipStream_t s);  // a query of a window: logits and statistics of J
 hipError_t launch_attn_dense_floor(const AttnArgs& a, int B, int n_slots, int wide, int idle_units, int writer, hipStream_t s);
 hipError_t launch_attn_ragged(const AttnArgs& d, const AttnArgs& f, bool balanced, hipStream_t s);  // d: planned dense, f: gather or compact

@@ -11,8 +11,9 @@
 //         4 jg + i - 4 of block B, where the first product left this lane's weights.  Product e of eight takes dim 8 m + e as its row m, so
 //         lane (jg, n) loads 16 bytes of a V row as they lie (dims 8 n .. + 7), and has dims 8 (4 jg + i) + e of column n in the end:
 //         maximum, sum and accumulator of a column stay in the lanes that have its logits.
-// A weight goes into the second product as the sum of two bf16 (what is lost is below 2^-17 of it): with one the output would
-// carry the weights' 2^-9, with two it has fp32's accuracy but for the order of the sums.
+// A weight goes into the second product as the sum of bf16 terms, each to nearest: with one the output would carry the weights' 2^-9.
+// Three hold all 24 bits, for launches whose time is the rows they read (few columns, own rows); two lose up to 2^-18 (1e-6 of an output),
+// where the third would cost a quarter of the matrix instructions (many columns).
 #include "sfi_internal.h"
 #include "sfi_wave.h"
 
@@ -146,20 +147,24 @@ __device__ __forceinline__ void mask(const Cols<NCB>& C, f32x4 (&s)[NCB][2], int
       s[cb][i >> 2][i & 3] = r >= C.lo[cb] && r < C.hi[cb] ? s[cb][i >> 2][i & 3] : -__builtin_inff();
     }
 }
-// The weights of a block of columns as two bf16 terms, and their sum over the lane's rows.
+// The weights of a block of columns in bf16 terms, and their sum over the lane's rows.
 struct Weights {
-  bf16x8 hi, lo;
+  bf16x8 hi, lo, rest;
 };
+template <bool THREE>
 __device__ __forceinline__ float weights_of(const f32x4 (&s)[2], float m, float c2, Weights& w) {
   float p[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -m));  // a masked row: 2^-inf = 0
-  uint32_t hi[4], lo[4];
+  uint32_t hi[4], lo[4], rest[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     hi[i] = round2(p[2 * i], p[2 * i + 1]);
-    lo[i] = round2(p[2 * i] - __uint_as_float(hi[i] << 16), p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
+    const float r0 = p[2 * i] - __uint_as_float(hi[i] << 16), r1 = p[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u);
+    lo[i] = round2(r0, r1);
+    if (THREE) rest[i] = round2(r0 - __uint_as_float(lo[i] << 16), r1 - __uint_as_float(lo[i] & 0xffff0000u));
   }
+  if (THREE) w.rest = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
   w.hi = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
   w.lo = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
   return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
@@ -168,13 +173,13 @@ __device__ __forceinline__ float weights_of(const f32x4 (&s)[2], float m, float 
 // from what fp32 or bf16 lose anything at) is it brought up, accumulators and sums rescaled and the weights made again.  That
 // happens in the first tile, whose maximum is kNeg, and rarely later; the common way looks for no maximum at all.  c2 > 0.
 constexpr float kLag = 256.f;
-template <int NCB>
+template <int NCB, bool THREE>
 __device__ __forceinline__ void soften(Cols<NCB>& C, const f32x4 (&s)[NCB][2], Weights (&w)[NCB], float c2) {
   float sum[NCB];
   bool up = false;
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) {
-    sum[cb] = weights_of(s[cb], C.m[cb], c2, w[cb]);
+    sum[cb] = weights_of<THREE>(s[cb], C.m[cb], c2, w[cb]);
     up |= sum[cb] > kLag;
   }
   if (__builtin_expect(__any(up), 0)) {
@@ -188,13 +193,13 @@ __device__ __forceinline__ void soften(Cols<NCB>& C, const f32x4 (&s)[NCB][2], W
       C.l[cb] *= f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) C.acc[cb][e] *= f;
-      sum[cb] = weights_of(s[cb], m1, c2, w[cb]);
+      sum[cb] = weights_of<THREE>(s[cb], m1, c2, w[cb]);
     }
   }
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) C.l[cb] += sum[cb];
 }
-// Products with V.
+// Products with V, two terms.
 __device__ __forceinline__ void add_rows(f32x4 (&acc)[8], const bf16x8 (&vt)[8], const Weights& w) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.hi, acc[e], 0, 0, 0);
@@ -265,7 +270,7 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
       }
       if (r0 < whole_from || r0 + kTile > whole_to) mask<NCB>(C, s, r0, jg);
       Weights w[NCB];
-      soften<NCB>(C, s, w, c2);
+      soften<NCB, true>(C, s, w, c2);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bf16x8 vt = turn_v(W[d].T.v, e);
@@ -273,6 +278,7 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
         for (int cb = 0; cb < NCB; ++cb) {
           C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].hi, C.acc[cb][e], 0, 0, 0);
           C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].lo, C.acc[cb][e], 0, 0, 0);
+          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].rest, C.acc[cb][e], 0, 0, 0);
         }
       }
       if (next < t1) issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
@@ -529,7 +535,7 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
         read_v(buf, vt);
         scores<NCB>(C, ka, kb, s);
         if (r0 + kTile > seen.least) mask<NCB>(C, s, r0, jg);
-        soften<NCB>(C, s, w, c2);
+        soften<NCB, false>(C, s, w, c2);
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb) add_rows(C.acc[cb], vt, w[cb]);
       }
