@@ -651,6 +651,7 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
   }
   __syncthreads();
   f32x4* s_o = reinterpret_cast<f32x4*>(lds);  // [lanes][quads]
+  bool odd = false;
   for (int g0 = 0; g0 < a.G; g0 += kRound) {
     const Share r = g0 == 0 ? first : share_of(g0);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -670,8 +671,35 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     if (r.rl == 0) {
       for (int k = 1; k < r.lanes; ++k) o += s_o[k * r.quads + r.item];
       store_out4(a.out, (head0 + r.g) * kHeadDim + 4 * r.c, make_float4(o[0], o[1], o[2], o[3]), a.out_bf16 != 0);
+      odd |= !(fabsf(o[0]) + fabsf(o[1]) + fabsf(o[2]) + fabsf(o[3]) < __builtin_inff());
     }
     __syncthreads();
+  }
+  // A column of the shared rows' launch takes the lead's rows behind those that its sequence shares with a weight of zero, which a V row with
+  // infinities or NaN turns into NaN.  An output that is not finite is therefore made again from the rows it sees alone, where others see more.
+  if (__builtin_expect(!__syncthreads_or(odd), 1)) return;
+  bool more = false;
+  for (int i = tid; i < a.B; i += kOwnThreads) more |= shared_of(a, i, len_of(a, i), len_of(a, a.lead)) > S;
+  if (!__syncthreads_or(more)) return;
+  start(C);
+  load_query(C.q[0], a.q + (head0 + min(n, a.G - 1)) * kHeadDim, n < a.G, jg);
+  for (int part = S > 0 ? 0 : 1; part < (S < L ? 2 : 1); ++part) {  // the lead's rows, then its own
+    Rows R = rows_of(a, part == 0 ? a.lead : b, h);
+    R.lo = C.lo[0] = part == 0 ? 0 : S;
+    C.hi[0] = part == 0 ? S : L;
+    R.hi = C.hi[0] - 1;
+    int reported = 0;
+    walk<1, kOwnWaves, 1, PAGED>(C, R, R.lo / kTile, R.hi / kTile + 1, R.lo, R.hi + 1, wave, jg, n, a.scale_log2, reported);
+  }
+  join<1, kOwnWaves, true>(C, wave, 16, 0, jg, n, lds, [&](int col) { return s_own[col]; });
+  __syncthreads();
+  for (int g0 = 0; g0 < a.G; g0 += kRound) {
+    const Share r = share_of(g0);  // the threads that stored before
+    if (r.rl != 0) continue;
+    const float4 v = *reinterpret_cast<const float4*>(&s_own[r.g][4 + 4 * r.c]);
+    const float z = s_own[r.g][1];
+    store_out4(a.out, (head0 + r.g) * kHeadDim + 4 * r.c, z > 0.f ? make_float4(v.x / z, v.y / z, v.z / z, v.w / z) : make_float4(0.f, 0.f, 0.f, 0.f),
+               a.out_bf16 != 0);
   }
 }
 

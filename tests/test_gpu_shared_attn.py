@@ -143,6 +143,38 @@ def test_a_scale_and_peaked_softmax():
     _run(4, 8, 2, [150, 160, 170, 128], [128] * 4, scale=1.5)
 
 
+@pytest.mark.parametrize("B, Hq, Hkv", [(3, 4, 2), (5, 5, 1), (6, 16, 1), (8, 32, 2), (20, 32, 2)])
+@pytest.mark.parametrize("layout", ["head", "htd"])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_rows_that_only_others_share_may_hold_anything(B, Hq, Hkv, layout, bad):
+    """Sequences that share less of the lead are not touched by what the rows behind their share hold, in K or in V."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    n, few = 700, [0, 1, 33, 416]
+    c = ref.Cache(B, Hkv, n + 20, layout, seed=61)
+    lens = [n + 1 + i % 9 for i in range(B)]
+    shared = [n if b in (0, 1) else few[b % 4] for b in range(B)]
+    K, V = to64(c.numpy(0)), to64(c.numpy(1))
+    row = np.full((Hkv, 128), 0x7FC1 if bad == "nan" else 0x7F80, np.uint16)
+    c.put(0, 0, 500, row), c.put(1, 0, 450, row), c.put(1, 0, 600, row)
+    ctx = c.context(Hq)
+    try:
+        q = torch.randn((B, Hq, 128), generator=torch.Generator().manual_seed(62)).to(torch.bfloat16).cuda()
+        out = torch.zeros((B, Hq, 128), device="cuda")
+        _step(f"B={B} heads {Hq}/{Hkv} {layout} {bad}")
+        sfi.sfi_shared_attn(ctx.handle, q, c.K, c.V, i32(lens), i32(shared), 0, n, 0, out)
+        torch.cuda.synchronize()
+        qn, got = to64(bits(q)), out.cpu().numpy().astype(np.float64)
+        assert not np.isfinite(got[:2]).any()
+        for b in range(2, B):
+            k, v = (np.concatenate((x[0, :, :shared[b]], x[b, :, shared[b]:lens[b]]), axis=1) for x in (K, V))
+            want, p, size = ref.attend(qn[b], k, v)
+            assert (np.abs(got[b] - want) <= ref.out_bound(p, v, Hq, size, want, False)).all(), b
+    finally:
+        ctx.close()
+
+
 def test_inputs_out_of_range_are_clamped_and_reported():
     _run(4, 8, 2, [200, 150, 100, 60], [200, 190, -5, 60], lead=1, max_shared=150, poison=False, status=32)
     _run(3, 8, 2, [200, 100, 90], [80, 80, 80], max_len=150, poison=False, status=1)
