@@ -385,15 +385,16 @@ typedef struct sfi_rope {
   int32_t scaling;      /* SFI_ROPE_* */
   int32_t orig_ctx;     /* TURNS, DIMS: rows of the context the model was trained on */
   double base;          /* > 1 */
-  double factor;        /* LINEAR, TURNS, DIMS: > 0 */
+  double factor;        /* LINEAR, TURNS, DIMS: 1e-9 to 1e9 */
   double low, high;     /* TURNS, DIMS: turns, 0 < low < high */
   double magnitude;     /* factor on sine and cosine; 0 selects 1 */
-  const double* freqs;  /* HOST [rot_dim / 2], read during the call, or NULL */
+  const double* freqs;  /* HOST [rot_dim / 2], |f| <= 1e9, read during the call, or NULL */
 } sfi_rope;
 /* The f_i of a rule -> freqs (HOST, [rot_dim / 2]).  Pure host arithmetic. */
 int sfi_rope_freqs(const sfi_rope* rope, double* freqs);
 /* The rule of this context's sfi_rope_append calls: a small table in the workspace, written by a kernel on `stream` (appends on other streams
- * must be ordered behind it).  Once per context, or whenever the rule changes; `rope` is read during the call only. */
+ * must be ordered behind it).  Once per context, or whenever the rule changes (an append that a graph has captured belongs to the rule of that time:
+ * capture it again); `rope` is read during the call only. */
 int sfi_set_rope(sfi_ctx* ctx, const sfi_rope* rope, void* stream);
 
 /*
@@ -406,7 +407,7 @@ int sfi_set_rope(sfi_ctx* ctx, const sfi_rope* rope, void* stream);
  *   q_out    bf16 [B, max_new, Hq, 128] contiguous; may be q itself where that is laid out alike, and may not overlap q otherwise.
  *   K, V     the cache as in the hot calls, written here.  n_new, pos: DEVICE int32 [B].
  * Padding (t >= n_new[b]) is not read, and q_out keeps what it holds there.  A row whose block id is out of range is not written.
- * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW).  Needs sfi_set_rope.
+ * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW).  Needs sfi_set_rope.  B * max_new up to 2^26 - 4.
  */
 int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* k, int64_t k_stride_b, int64_t k_stride_t,
                     const void* v, int64_t v_stride_b, int64_t v_stride_t, const int32_t* ctx_len, const int32_t* n_new, const int32_t* pos,
@@ -421,7 +422,10 @@ int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_s
  *   shared_len  DEVICE int32 [B], brought into [0, min(ctx_len[b], ctx_len[lead], max_shared)] (SFI_GUARD_SHARED); the lead's own entry may be
  *               anything in that range.
  *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
- * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums.
+ * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with more than 32
+ * queries of a KV head in the batch (B * G), the softmax weights of the shared rows to 2^-18 of themselves.  Rows that only other
+ * sequences share may hold anything.  The launch is sized for sequences with max_len - max_shared rows of their own or fewer; one with
+ * many more (a small shared_len beside a large max_shared) is computed by few workgroups, and has better a call of its own.
  */
 int sfi_shared_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* ctx_len, const int32_t* shared_len,
                     int32_t lead, int32_t max_shared, int32_t max_len, void* out, void* stream);
@@ -445,13 +449,14 @@ int sfi_weight_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, c
  *   kept[b, h, :]  = the rows of J that stay, ascending, entries behind n_kept[b, h] = min(budget, |J|) set to -1 (row stride `budget`)
  *   weights_out, row_pos_out: the kept rows' entries of weights and row_pos moved alike; weights_out is zero from ctx_len_out[b] on.
  * dst: the context of the cache that is written (strides, block table, max_ctx; the same batch and n_kv_heads; nothing else of it is used), which
- * may be ctx itself.  K_out == K and V_out == V evicts in place: strides and page size have to be the same, and a block table of dst must name the
- * same block at the same place or none of the sequence's.  Otherwise what is read and what is written may not overlap; rows of K_out, V_out behind
+ * may be ctx itself.  K_out == K and V_out == V evicts in place: strides and page size have to be the same, and an entry of dst's block table must name the
+ * block that the same entry of ctx's names or one that no sequence's rows are read from.  Otherwise what is read and what is written may not overlap; rows of K_out, V_out behind
  * ctx_len_out[b] are left as they are.
  * weights, row_pos: [B, Hkv, max_ctx of ctx] contiguous, weights_out, row_pos_out: [B, Hkv, max_ctx of dst].  row_pos (int32, any per-row
  * data, say each row's position) may be NULL, and so may row_pos_out, recent_start_out and weights_out, and kept with budget = 0;
  * ctx_len_out may be ctx_len, weights_out weights and row_pos_out row_pos (with equal max_ctx).  max_len: upper bound of ctx_len[] (0 = max_ctx); min(max_len,
- * n_sink + budget + recent) rows have to fit dst.  budget <= cfg.max_budget.
+ * n_sink + budget + recent) rows have to fit dst.  budget <= cfg.max_budget.  Uses the Selector's part of the workspace: evidence left there by
+ * sfi_slow_attn is gone afterwards.
  * Keys keep the positions they were rotated with: sfi_rope_append takes the next token's position in pos from then on, and index
  * sets (sel_idx) and compact buffers are stale.  Rows that several sequences share (sfi_shared_attn over one set of blocks) can be evicted from in
  * place only if they are sink rows, which never move.
@@ -478,7 +483,8 @@ enum {
   SFI_STAGE_COUNT = 4,    /* not used: always 0 */
   SFI_STAGE_WRITE = 5,    /* ordered index write; short J: the whole selection, with the scoring and the output's merge
                              where no SCORE stage ran in a slow step */
-  SFI_STAGE_ATTN2 = 6,    /* the fast sequences' attention of a mixed step, where it is a launch of its own */
+  SFI_STAGE_ATTN2 = 6,    /* the fast sequences' attention of a mixed step, where it is a launch of its own; sfi_shared_attn: the sequences' own
+                             rows, with the merge (the shared ones: ATTN) */
   SFI_STAGE_REORG = 7,    /* rows copied: compact-buffer gather, append of new rows, the kept rows of an eviction */
   SFI_N_STAGES = 8
 };

@@ -1384,6 +1384,9 @@ int sfi_query_splits(const sfi_ctx* x, int32_t* dense_splits, int32_t* fast_spli
 
 // ---- rotary positions, attention over shared rows and with running weights, eviction -------------------------------------------
 namespace {
+// The runtime counts the threads along one index of a grid in 32 bits: workgroups of 256.
+constexpr int64_t kMaxWorkgroups = ((int64_t)1 << 24) - 1;
+
 // What pair i turns per position, in radians (include/sfi.h has the formulas).
 int rope_freqs(const sfi_rope* r, double* f) {
   if (r == nullptr || f == nullptr) return SFI_EINVAL;
@@ -1401,7 +1404,7 @@ int rope_freqs(const sfi_rope* r, double* f) {
     return SFI_OK;
   }
   if (!(r->base > 1.0) || !(r->base <= 1e30)) return SFI_EINVAL;
-  if (r->scaling != SFI_ROPE_PLAIN && (!(r->factor > 0.0) || !(r->factor <= 1e9))) return SFI_EINVAL;
+  if (r->scaling != SFI_ROPE_PLAIN && (!(r->factor >= 1e-9) || !(r->factor <= 1e9))) return SFI_EINVAL;
   if (r->scaling == SFI_ROPE_TURNS || r->scaling == SFI_ROPE_DIMS) {
     if (r->orig_ctx < 1 || !(r->low > 0.0) || !(r->high > r->low) || !(r->high <= 1e30)) return SFI_EINVAL;
   } else if (r->scaling != SFI_ROPE_PLAIN && r->scaling != SFI_ROPE_LINEAR) {
@@ -1473,7 +1476,9 @@ int sfi_rope_append(sfi_ctx* x, const void* q, int64_t q_stride_b, int64_t q_str
                     int32_t max_new, void* q_out, void* K, void* V, void* stream) {
   if (x == nullptr || k == nullptr || v == nullptr || ctx_len == nullptr || K == nullptr || V == nullptr) return SFI_EINVAL;
   if ((q == nullptr) != (q_out == nullptr)) return SFI_EINVAL;
-  if (x->rope_dim == 0 || max_new < 1 || max_new > x->cfg.max_ctx) return SFI_EINVAL;
+  if (max_new < 1 || max_new > x->cfg.max_ctx) return SFI_EINVAL;
+  if (((int64_t)x->cfg.batch * max_new + 3) / 4 > kMaxWorkgroups) return SFI_EUNSUPPORTED;  // four rows each
+  if (x->rope_dim == 0) return SFI_EINVAL;
   if (x->cfg.page_size != 0 && x->table == nullptr) return SFI_EINVAL;  // paged cache without a block table
   const int64_t st[6] = {q != nullptr ? q_stride_b : 0, q != nullptr ? q_stride_t : 0, k_stride_b, k_stride_t, v_stride_b, v_stride_t};
   for (int i = 0; i < 6; ++i) {
@@ -1484,7 +1489,6 @@ int sfi_rope_append(sfi_ctx* x, const void* q, int64_t q_stride_b, int64_t q_str
       misaligned(ctx_len, 4) || misaligned(n_new, 4) || misaligned(pos, 4))
     return SFI_EALIGN;
   const sfi_config& c = x->cfg;
-  if ((int64_t)c.batch * max_new >= (int64_t)1 << 32) return SFI_EUNSUPPORTED;  // one workgroup per four tokens
   CallRecord call_record(x);
   RopeArgs a;
   memset(&a, 0, sizeof(a));
@@ -1594,7 +1598,7 @@ int sfi_evict(sfi_ctx* x, const void* K, const void* V, const int32_t* ctx_len, 
   CallRecord call_record(x);
   const int B = c.batch, nJ = ml - c.recent - c.n_sink;
   const int n_chunks = (most + kMoveRows - 1) / kMoveRows;
-  if (((int64_t)n_chunks + 1) * B * c.n_kv_heads > INT32_MAX) return SFI_EUNSUPPORTED;
+  if (((int64_t)n_chunks + 1) * B * c.n_kv_heads > kMaxWorkgroups) return SFI_EUNSUPPORTED;
   SelArgs sa;
   fill_sel(x, &sa, ctx_len, ml, nullptr, budget, 0, kept, n_kept);
   sa.weights = weights; sa.w_rows = c.max_ctx;

@@ -108,6 +108,18 @@ def test_append_refuses(ctx):
     # (with a rule: a context can only be given one where there is a device, so the checks behind that one run in the GPU tests too)
 
 
+def test_more_rows_than_a_launch_takes(ctx):
+    many = ctx(batch=1 << 15, max_ctx=4096)
+    assert _append(many, max_new=4096) == EUNSUPPORTED  # 2^27 rows
+    assert _append(many, max_new=0) == EINVAL and _append(many, max_new=4097) == EINVAL
+
+
+@pytest.mark.parametrize("factor", [0.0, 1e-300, 9e-10, 2e9, float("inf")])
+@pytest.mark.parametrize("scaling", [1, 2, 3])
+def test_factors_that_leave_no_angle(factor, scaling):
+    assert sfi.load_library().sfi_rope_freqs(C.byref(_rope(scaling=scaling, factor=factor)), (C.c_double * 64)()) == EINVAL
+
+
 def _rows(name, h, **over):
     lib = sfi.load_library()
     a = (dict(q=P, K=P, V=P, ctx_len=P, shared_len=P, lead=0, max_shared=64, max_len=0, out=P) if name == "sfi_shared_attn" else
