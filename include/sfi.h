@@ -423,9 +423,9 @@ int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_s
  *               anything in that range.
  *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
  * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with more than 32
- * queries of a KV head in the batch (B * G), the softmax weights of the shared rows to 2^-18 of themselves.  Rows that only other
- * sequences share may hold anything.  The launch is sized for sequences with max_len - max_shared rows of their own or fewer; one with
- * many more (a small shared_len beside a large max_shared) is computed by few workgroups, and has better a call of its own.
+ * queries of a KV head in the batch (B * G) and a bf16 output or max_shared >= 24576, the softmax weights of the shared rows to 2^-18 of themselves.  Rows that only other
+ * sequences share may hold anything.  Rows of their own are shared out to the compute units where the batch has few (sequence, KV head) pairs; where it
+ * has many, each is read by one workgroup, and a sequence with far more of them than the others has better a call of its own.  Row strides below 2^29.
  */
 int sfi_shared_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* ctx_len, const int32_t* shared_len,
                     int32_t lead, int32_t max_shared, int32_t max_len, void* out, void* stream);

@@ -1436,17 +1436,17 @@ void all_rows_view(const sfi_ctx* x, sfi_ctx* y) {
   y->cfg.selector_mode = 0;
   y->alpha = 1.0f;
 }
-// Splits of the shared rows (none where nothing can be shared) and of each sequence's own.
+// Splits of the shared rows (none where nothing can be shared): one workgroup per unit.  The sequences' own rows: three workgroups fit a unit and are shared
+// out where that is two per pair or more (32 sequences of 8 KV heads, 650 rows each: 27 us; four, five, eight per unit 33, 32, 33); below that one per
+// pair, which needs no records of its own (64 sequences, 33 to 512 rows: 27.5 us, two per pair 32, three 35).
 void shared_splits(const sfi_ctx* x, SharedArgs* a) {
   const int cols = shared_cols(a->B * a->G), groups = (a->B * a->G + cols - 1) / cols;
-  auto splits = [&](int tiles, int64_t cells, int wgs, int cap) {
-    int64_t s = wgs / cells;
-    s = std::min<int64_t>(s, (tiles + kWaves - 1) / kWaves);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, cap));
-  };
-  a->n_shared = a->max_shared > 0 ? splits((a->max_shared + kTile - 1) / kTile, (int64_t)a->Hkv * groups, x->n_cu, 40) : 0;
-  // three workgroups of the own rows' launch fit a unit; a wave has a tile at least
-  a->n_own = splits((a->len_cap - a->max_shared + kTile - 1) / kTile + 1, (int64_t)a->Hkv * a->B, 3 * x->n_cu, 20);
+  const int tiles = (a->max_shared + kTile - 1) / kTile;
+  const int64_t units = std::max<int64_t>(1, x->n_cu / ((int64_t)a->Hkv * groups));
+  a->n_shared = (int)std::min<int64_t>(std::min<int64_t>(units, kMaxSharedSplits), (tiles + kWaves - 1) / kWaves);
+  const int wgs = 3 * x->n_cu / a->Hkv;
+  const int own_tiles = (a->len_cap - a->max_shared + kTile - 1) / kTile + 1;
+  a->own_wgs = wgs >= 2 * a->B && a->B <= kMaxOwnPlan && own_tiles > kWaves ? std::min(wgs, a->B * ((own_tiles + kWaves - 1) / kWaves)) : 0;
 }
 }  // namespace
 
@@ -1518,7 +1518,7 @@ int sfi_shared_attn(sfi_ctx* x, const void* q, const void* K, const void* V, con
   if ((rc = resolve_max_len(x, max_len, &ml)) != SFI_OK) return rc;
   const sfi_config& c = x->cfg;
   if (lead < 0 || lead >= c.batch || max_shared < 0 || max_shared > ml) return SFI_EINVAL;
-  if ((int64_t)c.batch * x->G > INT32_MAX / 2) return SFI_EUNSUPPORTED;
+  if ((int64_t)c.batch * x->G > INT32_MAX / 2 || c.k_stride_t >= (int64_t)1 << 29 || c.v_stride_t >= (int64_t)1 << 29) return SFI_EUNSUPPORTED;  // four rows: 32 bits
   hipStream_t st = (hipStream_t)stream;
   CallRecord call_record(x);
   SharedArgs a;

@@ -264,6 +264,8 @@ struct MoveArgs {
 };
 
 // Dense attention of a batch that shares its first rows.
+constexpr int kMaxSharedSplits = 40;  // records a query head has of the shared rows, of kSlotCap
+constexpr int kMaxOwnPlan = 384;  // sequences whose own rows can be shared out (two workgroups each, three per unit)
 struct SharedArgs {
   const uint16_t* q;
   const uint16_t* K;
@@ -271,11 +273,12 @@ struct SharedArgs {
   int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;
   const int32_t* ctx_len;
   const int32_t* shared_len;
-  float* part;                   // records: splits [0, n_shared) of the shared rows, [n_shared, n_shared + n_own) of a sequence's own
+  float* part;                   // records: splits [0, n_shared) of the shared rows, those behind them of a sequence's own
   const int32_t* table;          // paged cache (see AttnArgs)
   int64_t table_stride;
   int32_t page_lg, page_rpb, n_blocks;
-  int32_t B, Hq, Hkv, G, lead, max_shared, len_cap, n_shared, n_own;
+  int32_t B, Hq, Hkv, G, lead, max_shared, len_cap, n_shared;
+  int32_t own_wgs;               // workgroups per KV head that the sequences' own rows are shared out to; 0: one per sequence
   float scale_log2;
   float* out;
   uint32_t* arrive;              // Workspace::arrive: the first counter of a pair counts its workgroups of the own rows' launch

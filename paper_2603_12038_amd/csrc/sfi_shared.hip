@@ -12,8 +12,10 @@
 //         lane (jg, n) loads 16 bytes of a V row as they lie (dims 8 n .. + 7), and has dims 8 (4 jg + i) + e of column n in the end:
 //         maximum, sum and accumulator of a column stay in the lanes that have its logits.
 // A weight goes into the second product as the sum of bf16 terms, each to nearest: with one the output would carry the weights' 2^-9.
-// Three hold all 24 bits, for launches whose time is the rows they read (few columns, own rows); two lose up to 2^-18 (1e-6 of an output),
-// where the third would cost a quarter of the matrix instructions (many columns).
+// Three hold all 24 bits; two lose up to 2^-18, 2.4e-6 of the outputs' norm at any length where the weights are alike.  Two are taken for many columns where
+// the third is not seen: behind it a bf16 output rounds by 2^-9, and from kTwoTermRows shared rows on an fp32 sum in row order loses as much (3e-7 at
+// 200 rows, 1.2e-6 at 16384, 2.2e-6 at 32768; with three terms here 2e-7, 3e-7, 4e-7).  Time with two / three terms: 64 sequences of 64 heads over
+// 32768 rows 103 / 126 us, over 2048 18.8 / 20.1; 32 of 32 over 16384 28.3 / 30.
 #include "sfi_internal.h"
 #include "sfi_wave.h"
 
@@ -199,12 +201,17 @@ __device__ __forceinline__ void soften(Cols<NCB>& C, const f32x4 (&s)[NCB][2], W
 #pragma unroll
   for (int cb = 0; cb < NCB; ++cb) C.l[cb] += sum[cb];
 }
-// Products with V, two terms.
+// Products with V.
+template <bool THREE>
 __device__ __forceinline__ void add_rows(f32x4 (&acc)[8], const bf16x8 (&vt)[8], const Weights& w) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.hi, acc[e], 0, 0, 0);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.lo, acc[e], 0, 0, 0);
+  if (THREE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[e], w.rest, acc[e], 0, 0, 0);
+  }
 }
 template <int NCB>
 __device__ __forceinline__ void start(Cols<NCB>& C) {
@@ -249,41 +256,51 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
       issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, td * kTile, jg, n);
     }
   }
-  for (; t < t1; t += DEPTH * NW) {
+  // Tile td out of buffer d, and the one that takes its place.
+  auto tile = [&](int d, int td, bool refill) {
+    const int next = td + DEPTH * NW, r0 = td * kTile;
+    f32x4 s[NCB][2];
+    {
+      bf16x8 ka[4], kb[4];
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const int td = t + d * NW, next = td + DEPTH * NW, r0 = td * kTile;
-      if (td >= t1) break;
-      f32x4 s[NCB][2];
-      {
-        bf16x8 ka[4], kb[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          ka[k] = __builtin_bit_cast(bf16x8, W[d].T.ka[k]);
-          kb[k] = __builtin_bit_cast(bf16x8, W[d].T.kb[k]);
-        }
-        scores<NCB>(C, ka, kb, s);
+      for (int k = 0; k < 4; ++k) {
+        ka[k] = __builtin_bit_cast(bf16x8, W[d].T.ka[k]);
+        kb[k] = __builtin_bit_cast(bf16x8, W[d].T.kb[k]);
       }
-      if (next < t1) {
-        W[d].place(R, next, bad);
-        issue_k<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
-      }
-      if (r0 < whole_from || r0 + kTile > whole_to) mask<NCB>(C, s, r0, jg);
-      Weights w[NCB];
-      soften<NCB, true>(C, s, w, c2);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bf16x8 vt = turn_v(W[d].T.v, e);
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb) {
-          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].hi, C.acc[cb][e], 0, 0, 0);
-          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].lo, C.acc[cb][e], 0, 0, 0);
-          C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].rest, C.acc[cb][e], 0, 0, 0);
-        }
-      }
-      if (next < t1) issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
+      scores<NCB>(C, ka, kb, s);
     }
+    if (refill) {
+      W[d].place(R, next, bad);
+      issue_k<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
+    }
+    if (r0 < whole_from || r0 + kTile > whole_to) mask<NCB>(C, s, r0, jg);
+    Weights w[NCB];
+    soften<NCB, true>(C, s, w, c2);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bf16x8 vt = turn_v(W[d].T.v, e);
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb) {
+        C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].hi, C.acc[cb][e], 0, 0, 0);
+        C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].lo, C.acc[cb][e], 0, 0, 0);
+        C.acc[cb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w[cb].rest, C.acc[cb][e], 0, 0, 0);
+      }
+    }
+    if (refill) issue_v<PAGED>(W[d].T, R, W[d].A, W[d].B, next * kTile, jg, n);
+  };
+  if (DEPTH == 1) {
+    for (; t < t1; t += NW) tile(0, t, t + NW < t1);
+    return;
   }
+  // A loop in which every request is made, and the last tiles behind it: with a branch around requests the compiler waits for all that are on
+  // their way (32768 rows of 8 heads, 16 / 32 columns: 26.3 / 30.4 us, without the branch 25.1 / 29.8; paged, 65536 rows: 47 / 45 us, 6.0 TB/s).
+  for (; t + (2 * DEPTH - 1) * NW < t1; t += DEPTH * NW) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) tile(d, t + d * NW, true);
+  }
+#pragma unroll
+  for (int d = 0; d < 2 * DEPTH - 1; ++d)
+    if (t + d * NW < t1) tile(d % DEPTH, t + d * NW, t + (d + DEPTH) * NW < t1);
 }
 
 // Joins the columns of the NR waves that had other rows of the same columns (rank: which of them this wave is, 0 .. NR - 1; cols: the columns of all
@@ -436,12 +453,13 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
 //   stage.  In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read
 //   together, one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of
 //   four rows), lies in different banks.
-// - Eight waves, two on each SIMD.  64 sequences of 64 heads over 32768 rows: 105 to 110 us, 69.3 GFLOP and half as many again for the weights' second terms,
-//   950 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200; the matrix pipe is busy 46 % of the time, the vector
-//   pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's products with V beside stage t + 1's
-//   weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.  32 sequences of 32
-//   heads over 16384 rows, paged (128 columns): 29 us for 134 MB, 4.7 TB/s, and 17 MB of records.
-template <int NCB, int CG, int RG, bool PAGED>
+// - Eight waves, two on each SIMD.  64 sequences of 64 heads over 32768 rows of 8 KV heads: 100 to 106 us, 69.3 GFLOP and half as many again for the
+//   weights' second terms, 1000 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200; the matrix pipe is busy 46 % of the time,
+//   the vector pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's products with V beside
+//   stage t + 1's weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.  32 sequences of
+//   32 heads over 16384 rows, paged (128 columns): 27 us for 67 MB: 12 us for the first rows and the records (17 MB), then 1.9 us for 64 rows of each
+//   split, of which two waves' 96 matrix instructions are 0.64.
+template <int NCB, int CG, int RG, bool THREE, bool PAGED>
 __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
   constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
@@ -474,20 +492,25 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
     const int last = most - 1;
     const int my_row = tid >> 4, piece = tid & 15;
     uint4 pk[kAhead][kLoads], pv[kAhead][kLoads];
+    // A wave's 64 pieces are of four rows, which lie in one page.
+    auto row_of = [&](int t, int j) { return min(t * kRowsHere + 4 * wave + j * kRowStep, last); };
+    int page[kLoads];  // of the stage that is requested next
+    auto look_up = [&](int t) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) page[j] = PAGED ? R.table[row_of(t, j) >> R.lg] : 0;
+    };
     auto request = [&](int slot, int t) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
-        const int row = min(t * kRowsHere + my_row + j * kRowStep, last);
+        int row = row_of(t, j);
+        const uint32_t more = (uint32_t)min(lane >> 4, last - row);
         if (PAGED) {
-          const int page = R.table[row >> R.lg], pc = min(max(page, 0), R.n_blocks - 1);
-          bad |= pc != page ? kGuardBlock : 0;
-          const uint32_t at = (uint32_t)(pc * R.rpb + (row & ((1 << R.lg) - 1)));
-          pk[slot][j] = load16<false>(R.K + (uint64_t)at * R.k_st + piece * 16);
-          pv[slot][j] = load16<false>(R.V + (uint64_t)at * R.v_st + piece * 16);
-        } else {  // a KV head's rows lie within 4 GiB
-          pk[slot][j] = load16<false>(R.K + ((uint32_t)row * (uint32_t)R.k_st + piece * 16));
-          pv[slot][j] = load16<false>(R.V + ((uint32_t)row * (uint32_t)R.v_st + piece * 16));
+          const int pc = min(max(page[j], 0), R.n_blocks - 1);
+          bad |= pc != page[j] ? kGuardBlock : 0;
+          row = pc * R.rpb + (row & ((1 << R.lg) - 1));
         }
+        pk[slot][j] = load16<false>(R.K + (uint64_t)(uint32_t)row * R.k_st + (more * (uint32_t)R.k_st + piece * 16));
+        pv[slot][j] = load16<false>(R.V + (uint64_t)(uint32_t)row * R.v_st + (more * (uint32_t)R.v_st + piece * 16));
       }
     };
     auto stash = [&](int slot, int buf) {
@@ -518,49 +541,122 @@ __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const Shar
       }
     };
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) request(s, min(t0 + s, t1 - 1));
+    for (int s = 0; s < kAhead; ++s) {
+      look_up(min(t0 + s, t1 - 1));
+      request(s, min(t0 + s, t1 - 1));
+      __builtin_amdgcn_sched_barrier(0);  // in this order: the loop's wait for the first stage is not one for all of them
+    }
+    look_up(min(t0 + kAhead, t1 - 1));
     f32x4 s[NCB][2];
     bf16x8 ka[4], kb[4], vt[8];
     Weights w[NCB];
-    for (int tt = t0; tt < t1; tt += kAhead) {
+    auto stage = [&](int t, int u) {
+      const int r0 = t * kRowsHere + rg * kTile, buf = u * kStage;
+      stash(u, buf);
+      request(u, min(t + kAhead, t1 - 1));
+      look_up(min(t + kAhead + 1, t1 - 1));
+      __syncthreads();
+      read_k(buf, ka, kb);
+      read_v(buf, vt);
+      scores<NCB>(C, ka, kb, s);
+      if (r0 + kTile > seen.least) mask<NCB>(C, s, r0, jg);
+      soften<NCB, THREE>(C, s, w, c2);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = tt + u;
-        if (t >= t1) break;
-        const int r0 = t * kRowsHere + rg * kTile, buf = u * kStage;
-        stash(u, buf);
-        request(u, min(t + kAhead, t1 - 1));
-        __syncthreads();
-        read_k(buf, ka, kb);
-        read_v(buf, vt);
-        scores<NCB>(C, ka, kb, s);
-        if (r0 + kTile > seen.least) mask<NCB>(C, s, r0, jg);
-        soften<NCB, false>(C, s, w, c2);
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb) add_rows(C.acc[cb], vt, w[cb]);
-      }
+      for (int cb = 0; cb < NCB; ++cb) add_rows<THREE>(C.acc[cb], vt, w[cb]);
+    };
+    int t = t0;
+    for (; t + 1 < t1; t += kAhead) {  // (no way out in the middle: it would make the compiler wait for both stages at the head)
+      stage(t, 0);
+      stage(t + 1, 1);
     }
+    if (t < t1) stage(t, 0);
   }
   if (RG > 1) __syncthreads();  // the buffers are read no more
   join<NCB, RG, false>(C, rg, kCols, c0, jg, n, reinterpret_cast<float*>(lds), [&](int col) { return shared_record(a, c_first + col, h, split); });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
-// A sequence's own rows: n_own workgroups per KV head and sequence, and the merge.  The last of a pair's workgroups to finish merges the
-// records of all and those of the shared rows, which the launch before has left, into the output; records go from workgroup to workgroup at
-// device scope (stores and loads that name it, a count once the stores have been performed; the counter is zero between launches).
-// A pair with one workgroup keeps its record in LDS, and requests the shared rows' records before its waves are joined.
 constexpr int kOwnWaves = 4;
 constexpr int kOwnThreads = 64 * kOwnWaves;
 constexpr int kOwnAhead = 8;  // records a thread requests together
 constexpr int kDeviceScope = 16;  // cache-policy bit sc1 of the buffer instructions
+
+// Sequences that differ are evened out here rather than split alike: 100 to 1201 rows 32 us split alike, 30 shared out; all 650 27 both ways; one that shares
+// nothing among 31 that share 16384 rows is read by as many workgroups as it has records left, not by three.
+// Which part of whose own rows workgroup `slot` of a KV head has, of own_wgs: tiles shared out evenly over the batch, as few to a workgroup as
+// the workgroups allow (at least one for each wave), every sequence at least one workgroup and at most as many as it has records.
+struct OwnShare {
+  int b, part, parts;  // b = B: nothing
+};
+constexpr int kOwnPlan = kMaxOwnPlan / 64;  // sequences per lane
+__device__ __forceinline__ OwnShare own_share(const SharedArgs& a, int slot, int lane) {
+  const int L_lead = len_of(a, a.lead);
+  uint32_t tiles[kOwnPlan], total = 0u;
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < kOwnPlan; ++i) {
+    tiles[i] = 0u;
+    const int b = 64 * i + lane;
+    if (64 * i >= a.B || b >= a.B) continue;
+    const int L = len_of(a, b), S = shared_of(a, b, L, L_lead);
+    tiles[i] = S < L ? (uint32_t)((L + kTile - 1) / kTile - S / kTile) : 0u;
+    total += tiles[i];
+    most = fmaxf(most, (float)tiles[i]);
+  }
+  total = wave_sum(total);  // (the workspace has four bytes per row: below 2^32 tiles)
+  const uint32_t cap = kSlotCap - a.n_shared, longest = (uint32_t)(wave_max(most) * 1.000001f) + 1u;  // a float is off by 2^-24 of itself
+  const uint32_t lo = max(max((uint32_t)kOwnWaves, total / (uint32_t)a.own_wgs), longest / cap + 1u);
+  const uint32_t hi = total / (uint32_t)(a.own_wgs - a.B) + 1u;
+  auto parts_of = [&](uint32_t n, uint32_t per) { return max((n + per - 1u) / per, 1u); };
+  auto needed = [&](uint32_t per) {
+    uint32_t n = 0u;
+#pragma unroll
+    for (int i = 0; i < kOwnPlan; ++i)
+      if (64 * i < a.B) n += 64 * i + lane < a.B ? parts_of(tiles[i], per) : 0u;
+    return wave_sum(n);
+  };
+  uint32_t per = max(lo, hi);
+  constexpr int kTries = 6;
+  if (hi > lo) {
+    uint32_t n[kTries];
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) n[k] = needed(lo + (hi - lo) * k / kTries);
+#pragma unroll
+    for (int k = kTries - 1; k >= 0; --k) per = n[k] <= (uint32_t)a.own_wgs ? lo + (hi - lo) * k / kTries : per;
+  }
+  // (hi is enough: the sum of the rounded-up quotients is below total / hi + B)
+  uint32_t base = 0u;
+#pragma unroll
+  for (int i = 0; i < kOwnPlan; ++i) {
+    if (64 * i >= a.B) break;
+    const uint32_t mine = 64 * i + lane < a.B ? parts_of(tiles[i], per) : 0u, upto = base + wave_incl_scan(mine);
+    const uint64_t past = __ballot(upto > (uint32_t)slot);
+    if (past != 0ull) {
+      const int at = __builtin_ctzll(past);
+      const int parts = __builtin_amdgcn_readlane((int)mine, at);
+      return {64 * i + at, slot - (__builtin_amdgcn_readlane((int)upto, at) - parts), parts};
+    }
+    base = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  return {a.B, 0, 0};
+}
+
+// A sequence's own rows, one (ALONE) or several workgroups per KV head and sequence, and the merge.  Bound by the rows: 85 MB of 32 sequences (100 to 1201
+// rows of 8 KV heads, paged) in 30 us, 24 without the 17 MB of shared rows' records; 157 MB (1201 rows each) in 40 us, 4.4 TB/s with the records.
+// A tile per wave on its way: with two 48 us, as only two workgroups fit a unit then.  The last of a pair's workgroups to finish merges the
+// records of all and those of the shared rows, which the launch before has left, into the output; records go from workgroup to workgroup at
+// device scope (stores and loads that name it, a count once the stores have been performed; the counter is zero between launches).
+// A pair with one workgroup keeps its record in LDS, and requests the shared rows' records before its waves are joined.
 template <bool PAGED, bool ALONE>
 __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedArgs a) {
   __shared__ __align__(16) float lds[join_floats<kOwnWaves>(16)];
   __shared__ __align__(16) float s_own[16][kPartStride];
   __shared__ float s_w[16][kSlotCap];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, jg = lane >> 4, n = lane & 15;
-  const int h = blockIdx.x, split = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.x;
+  const OwnShare own = ALONE ? OwnShare{(int)blockIdx.y, 0, 1} : own_share(a, blockIdx.y, lane);
+  const int b = own.b;
+  if (!ALONE && b == a.B) return;
   const int64_t head0 = (int64_t)b * a.Hq + h * a.G;
   Cols<1> C;
   start(C);
@@ -574,14 +670,14 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     R.lo = S;
     R.hi = L - 1;
     const int first = S / kTile, tiles = (L + kTile - 1) / kTile - first;
-    walk<1, kOwnWaves, 1, PAGED>(C, R, first + (int)((int64_t)tiles * split / a.n_own), first + (int)((int64_t)tiles * (split + 1) / a.n_own), S, L, wave, jg, n,
+    walk<1, kOwnWaves, 1, PAGED>(C, R, first + (int)((int64_t)tiles * own.part / own.parts), first + (int)((int64_t)tiles * (own.part + 1) / own.parts), S, L, wave, jg, n,
                                  a.scale_log2, bad);
   }
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 
   // headers of a wave's heads, a record per lane; four output dims of every lanes-th record per thread, up to kRound heads at a time
   constexpr int kRec = kPartStride * (int)sizeof(float), kHeads = 16 / kOwnWaves, kRound = kOwnThreads / (kHeadDim / 4);
-  const int n_rec = a.n_shared + (ALONE ? 0 : a.n_own);  // in memory
+  const int n_rec = a.n_shared + (ALONE ? 0 : own.parts);  // in memory
   float* const pair = a.part + head0 * kSlotCap * kPartStride;
   const __amdgpu_buffer_rsrc_t recs = __builtin_amdgcn_make_buffer_rsrc(pair, 0, a.G * kSlotCap * kRec, 0x00020000);
   struct Share {
@@ -625,7 +721,7 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
   if (!ALONE) {
     for (int i = tid; i < a.G * (kPartStride / 4); i += kOwnThreads) {
       const int g = i / (kPartStride / 4), c4 = i % (kPartStride / 4);
-      __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(&s_own[g][4 * c4]), recs, (g * kSlotCap + a.n_shared + split) * kRec + 16 * c4, 0,
+      __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(&s_own[g][4 * c4]), recs, (g * kSlotCap + a.n_shared + own.part) * kRec + 16 * c4, 0,
                                              kDeviceScope);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's record stores have been performed
@@ -634,7 +730,7 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     uint32_t* const arrive = a.arrive + ((int64_t)b * a.Hkv + h) * kWaves * kArriveStride;
     if (tid == 0) s_before = __hip_atomic_fetch_add(arrive, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    if (s_before != (uint32_t)a.n_own - 1) return;
+    if (s_before != (uint32_t)own.parts - 1) return;
     if (tid == 0) __hip_atomic_store(arrive, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     request_headers();
     request(first, first.rl);
@@ -711,29 +807,37 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     else hipLaunchKernelGGL((kernel<__VA_ARGS__, false>), grid, dim3(threads), 0, s, a);                                    \
   } while (0)
 
+constexpr int kTwoTermRows = 24576;
 int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 32 ? 32 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256; }
 
 hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
   const int cols = shared_cols(a.B * a.G);
   const dim3 grid(a.Hkv, a.n_shared, (a.B * a.G + cols - 1) / cols);
+  const bool three = a.out_bf16 == 0 && a.max_shared < kTwoTermRows;
   switch (cols) {
     case 16: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 1); break;
     case 32: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 2); break;
-    case 64: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2); break;
-    case 128: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2); break;
-    default: SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1);
+    case 64:
+      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, true);
+      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, false);
+      break;
+    case 128:
+      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2, true);
+      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2, false);
+      break;
+    default:
+      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, true);
+      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, false);
   }
   return hipGetLastError();
 }
 hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s) {
-  const dim3 grid(a.Hkv, a.n_own, a.B);
-  if (a.n_own == 1) {
-    if (a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, true>), grid, dim3(kOwnThreads), 0, s, a);
-    else hipLaunchKernelGGL((own_rows_kernel<false, true>), grid, dim3(kOwnThreads), 0, s, a);
-  } else {
-    if (a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, false>), grid, dim3(kOwnThreads), 0, s, a);
-    else hipLaunchKernelGGL((own_rows_kernel<false, false>), grid, dim3(kOwnThreads), 0, s, a);
-  }
+  const bool alone = a.own_wgs == 0;
+  const dim3 grid(a.Hkv, alone ? a.B : a.own_wgs), block(kOwnThreads);
+  if (alone && a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, true>), grid, block, 0, s, a);
+  else if (alone) hipLaunchKernelGGL((own_rows_kernel<false, true>), grid, block, 0, s, a);
+  else if (a.table != nullptr) hipLaunchKernelGGL((own_rows_kernel<true, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((own_rows_kernel<false, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

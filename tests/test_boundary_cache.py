@@ -152,6 +152,14 @@ def test_no_context_or_no_block_table(ctx, name):
     assert _rows(name, ctx(**PAGED)) == EINVAL
 
 
+def test_shared_attention_takes_four_rows_within_32_bits(ctx):
+    lib = sfi.load_library()
+    for over in (dict(k_stride_t=1 << 29), dict(v_stride_t=1 << 29)):
+        h = ctx(**{**PAGED, **over})
+        assert lib.sfi_set_block_table(h, P, 256, 4) == OK
+        assert _rows("sfi_shared_attn", h) == EUNSUPPORTED
+
+
 def _evict(h, to, **over):
     a = dict(K=P, V=P, ctx_len=P, max_len=0, budget=64, weights=P, row_pos=P, dst=to, K_out=2 * P, V_out=2 * P, ctx_len_out=P, recent_start_out=P,
              weights_out=2 * P, row_pos_out=2 * P, kept=P, n_kept=P)

@@ -117,6 +117,19 @@ def test_tables_that_name_the_same_blocks():
         assert out.isfinite().all()
 
 
+@pytest.mark.parametrize("layout", ["head", "htd"])
+@pytest.mark.parametrize("B, Hq, Hkv, most", [(1, 8, 1, 6000), (3, 4, 2, 3000), (13, 8, 4, 1500), (40, 8, 4, 900), (130, 2, 1, 500)])
+def test_own_rows_of_very_different_lengths(B, Hq, Hkv, most, layout):
+    """None, a few, and many rows of their own, shared out to workgroups together; one sequence shares nothing."""
+    own = [(i * 7919) % most if i % 3 else i % 5 for i in range(B)]
+    own[B // 2] = most
+    shared = [100 - (i % 4) * 3 for i in range(B)]
+    shared[0] = 100
+    if B > 2:
+        shared[1] = 0
+    _run(B, Hq, Hkv, [s + o for s, o in zip(shared, own)], shared, layout=layout, poison=B < 40)
+
+
 def test_same_as_dense_attention_where_the_rows_are_the_same():
     import torch
     import paper_2603_12038_amd as sfi
