@@ -1604,7 +1604,9 @@ int sfi_evict(sfi_ctx* x, const void* K, const void* V, const int32_t* ctx_len, 
   sa.weights = weights; sa.w_rows = c.max_ctx;
   sa.guard = x->ws.guard;
   if (in_place) { sa.moved = x->ws.moved; sa.moved_words = 1 + B * c.n_kv_heads * n_chunks; }
-  if (nJ <= kPickMax) {
+  // Up to twice the usual length one launch also takes the keys from registers; worth it where the pairs keep the units busy: 24000 / 32000 rows, 32 pairs
+  // 16.4 / 17.4 us (the three launches 14.8 / 14.9), 128 pairs 18.6 / 20.6 (22.4 / 27.2), 256 pairs 18.9 / 21.3 (30 / 36.7).
+  if (nJ <= (4 * B * c.n_kv_heads >= x->n_cu ? 2 : 1) * kPickMax) {
     StageTimer t(x, st, SFI_STAGE_WRITE);
     SFI_TRY(launch_sel_pick(sa, B, nJ, 3, st));
     if (!t.stop()) return SFI_ELAUNCH;

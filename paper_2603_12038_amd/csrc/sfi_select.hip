@@ -349,6 +349,29 @@ __global__ __launch_bounds__(kSelThreads) void sel_finalize_kernel(const SelArgs
 // ---- running weights (eviction by accumulated attention weight) ------------------------------------------
 // A weight's ranking key: its bit pattern, which orders like the value; what is not above zero (a negative, NaN) counts as zero.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.f ? __float_as_uint(w) : 0u; }
+// Keys of N positions of J, four to a load wherever the rows begin: p0 .. p0 + 3, p0 + STEP .. p0 + STEP + 3, ...
+template <int N, int STEP>
+__device__ __forceinline__ void weight_keys(const SelArgs& a, const Cell& c, int p0, int nJ, uint32_t (&key)[N]) {
+  typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+  const float* w = a.weights + (int64_t)c.bh * a.w_rows + a.n_sink;
+  if (nJ < 4) {  // workgroup-uniform
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = p0 + i < nJ ? weight_key(w[p0 + i]) : 0u;
+    return;
+  }
+  four v[N / 4];
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) v[q] = *reinterpret_cast<const four*>(w + min(p0 + STEP * q, nJ - 4));
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) {
+    const int p = p0 + STEP * q, late = p - (nJ - 4);  // places the load was moved forward by, where it would have passed the end
+    if (late == 1) v[q] = four{v[q][1], v[q][2], v[q][3], 0.f};
+    if (late == 2) v[q] = four{v[q][2], v[q][3], 0.f, 0.f};
+    if (late == 3) v[q] = four{v[q][3], 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[4 * q + i] = p + i < nJ ? weight_key(v[q][i]) : 0u;
+  }
+}
 // What the launch behind the selecting ones needs, left by the first that reads the weights: the length as it was read (the
 // caller's ctx_len is overwritten in that launch), and its counters at zero.
 __device__ __forceinline__ void note_weights(const SelArgs& a, const Cell& c, int tid, int first, int step) {
@@ -374,16 +397,10 @@ __global__ __launch_bounds__(kSelThreads) void sel_weights_kernel(const SelArgs 
   if (p_lo >= nJ) return;
   __shared__ uint32_t s_hist[kHistBins / 2];
   uint32_t* keys = a.keys + (int64_t)c.bh * a.ld_pos;
-  const float* w = a.weights + (int64_t)c.bh * a.w_rows + a.n_sink;
   s_hist[tid] = 0u;
   uint32_t k[2][4];
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int p = p_lo + r * (kSelSeg / 2) + tid * 4 + i;
-      k[r][i] = p < nJ ? weight_key(w[p]) : 0u;
-    }
+  for (int r = 0; r < 2; ++r) weight_keys<4, 4>(a, c, p_lo + r * (kSelSeg / 2) + tid * 4, nJ, k[r]);
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
@@ -660,7 +677,8 @@ __global__ __launch_bounds__(kFuseThreads) void sel_fuse_kernel(const SelArgs a)
 // ---- short J: one workgroup per pair selects --------------------------------------------------------
 // SRC 0: the keys a scoring launch left; 1: straight from the logits (scoring included; workgroups of places > 0 merge the
 // dense records, four query heads each); 2: the accumulated evidence of a window; 3: running weights.
-// A thread holds P consecutive positions in registers.  The three radix passes run on LDS histograms over all of J;
+// A thread holds P positions in registers.  Weights: 16 x 6000 rows of 8 KV heads 7.5 us, 4 x 15900 10.3 (positions of a thread in a row, four bytes to a
+// load: 9.8 and 15.3); most of it the three passes over a thread's keys.  The three radix passes run on LDS histograms over all of J;
 // no list of candidates, no global histogram.
 template <int P, int SRC, bool LIST, int GT>
 __global__ __launch_bounds__(kPickThreads) void sel_pick_kernel(const SelArgs a) {
@@ -683,7 +701,9 @@ __global__ __launch_bounds__(kPickThreads) void sel_pick_kernel(const SelArgs a)
     const int nJ = nJ_of(a, c);
     const uint32_t ksel = ksel_of(a, nJ);
     int32_t* out = a.sel_idx + (int64_t)c.bh * a.budget;
-    const int p0 = tid * P;
+    // A thread's positions follow one another, or (weights) lie four by four in its wave's 64 P: one load of a wave is one piece of the row.
+    const int p0 = SRC == 3 ? (tid >> 6) * 64 * P + 4 * (tid & 63) : tid * P;
+    auto at = [&](int i) { return SRC == 3 ? p0 + 256 * (i / 4) + i % 4 : p0 + i; };
     uint32_t key[P];
     if (SRC == 1) {
       constexpr int NQ = P / 4;
@@ -701,9 +721,7 @@ __global__ __launch_bounds__(kPickThreads) void sel_pick_kernel(const SelArgs a)
 #pragma unroll
       for (int i = 0; i < P; ++i) key[i] = p0 + i < nJ ? __float_as_uint(f[i / 4][i % 4]) : 0u;
     } else if (SRC == 3) {
-      const float* w = a.weights + (int64_t)c.bh * a.w_rows + a.n_sink + p0;
-#pragma unroll
-      for (int i = 0; i < P; ++i) key[i] = p0 + i < nJ ? weight_key(w[i]) : 0u;
+      weight_keys<P, 256>(a, c, p0, nJ, key);
       note_weights(a, c, tid, place.i * kPickThreads, kPickThreads);
       for (int i = tid; i < (4096 + 1024 + 512) / 4; i += kPickThreads) reinterpret_cast<uint4*>(s_h)[i] = make_uint4(0u, 0u, 0u, 0u);
       __syncthreads();
@@ -731,36 +749,64 @@ __global__ __launch_bounds__(kPickThreads) void sel_pick_kernel(const SelArgs a)
     }
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (p0 + i < nJ) atomicAdd(&s_h[min(key[i] >> 19, 4095u)], 1u);
+      if (at(i) < nJ) atomicAdd(&s_h[min(key[i] >> 19, 4095u)], 1u);
     __syncthreads();
     find_kth_desc_lds<kPickThreads, 4096 / kPickThreads>(s_h, 4096, ksel, s_res, s_scr[0]);
     const uint32_t bin1 = s_res[0], k1 = s_res[1];
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (p0 + i < nJ && (key[i] >> 19) == bin1) atomicAdd(&s_h[4096 + ((key[i] >> 9) & 1023u)], 1u);
+      if (at(i) < nJ && (key[i] >> 19) == bin1) atomicAdd(&s_h[4096 + ((key[i] >> 9) & 1023u)], 1u);
     __syncthreads();
     find_kth_desc_lds<kPickThreads, 1>(s_h + 4096, 1024, k1, s_res, s_scr[1]);
     const uint32_t top22 = bin1 << 10 | s_res[0], k2 = s_res[1];
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (p0 + i < nJ && (key[i] >> 9) == top22) atomicAdd(&s_h[4096 + 1024 + (key[i] & 511u)], 1u);
+      if (at(i) < nJ && (key[i] >> 9) == top22) atomicAdd(&s_h[4096 + 1024 + (key[i] & 511u)], 1u);
     __syncthreads();
     find_kth_desc_lds<kPickThreads, 1>(s_h + 4096 + 1024, 512, k2, s_res, s_scr[2]);
     const uint32_t tau = top22 << 9 | s_res[0], take = s_res[1];
     uint32_t cg = 0, ce = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      if (p0 + i < nJ) {
+      if (at(i) < nJ) {
         cg += key[i] > tau;
         ce += key[i] == tau;
       }
     }
     uint32_t total;
-    const uint32_t ex = block_excl_scan<kPickThreads>(cg | ce << 16, s_scr[3], &total);  // both at most 16384
+    const uint32_t ex = block_excl_scan<kPickThreads>(cg | ce << 16, s_scr[3], &total);  // both at most 32768
     uint32_t gt = ex & 0xffffu, eq = ex >> 16;
+    if (SRC == 3) {
+      // (ex of the wave's first thread, then quad by quad: the lanes before this one, the quads before this one)
+      uint32_t before = (uint32_t)__builtin_amdgcn_readfirstlane((int)ex);
+#pragma unroll
+      for (int q = 0; q < P / 4; ++q) {
+        uint32_t n = 0u;
+#pragma unroll
+        for (int i = 4 * q; i < 4 * q + 4; ++i)
+          if (at(i) < nJ) n += (uint32_t)(key[i] > tau) | (uint32_t)(key[i] == tau) << 16;
+        const uint32_t upto = wave_incl_scan(n);
+        gt = (before + upto - n) & 0xffffu;
+        eq = (before + upto - n) >> 16;
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+#pragma unroll
+        for (int i = 4 * q; i < 4 * q + 4; ++i) {
+          if (at(i) < nJ) {
+            const bool g = key[i] > tau, e = key[i] == tau;
+            if (g || (e && eq < take)) {
+              const uint32_t pos = gt + min(eq, take);
+              if (pos < ksel) out[pos] = a.n_sink + at(i);
+            }
+            gt += g;
+            eq += e;
+          }
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      if (p0 + i < nJ) {
+      if (at(i) < nJ) {
         const bool g = key[i] > tau, e = key[i] == tau;
         if (g || (e && eq < take)) {
           const uint32_t pos = gt + min(eq, take);
@@ -1263,7 +1309,8 @@ hipError_t launch_sel_pick(SelArgs a, int B, int nJ, int src, hipStream_t s) {
   } else if (src == 2) {
     launch_pick_keys_t<2, false>(a, nJ, grid, s);
   } else if (src == 3) {
-    launch_pick_keys_t<3, false>(a, nJ, grid, s);
+    if (nJ <= kPickMax) launch_pick_keys_t<3, false>(a, nJ, grid, s);
+    else hipLaunchKernelGGL((sel_pick_kernel<32, 3, false, 1>), grid, dim3(kPickThreads), 0, s, a);
   } else {
     if (list) launch_pick_keys_t<0, true>(a, nJ, grid, s);
     else launch_pick_keys_t<0, false>(a, nJ, grid, s);

@@ -121,6 +121,20 @@ def test_lengths_where_the_selecting_launch_changes(n):
     _run(1, 2, [n + 20], 777, kind="ties")
 
 
+@pytest.mark.parametrize("n, kind", [(16385, "ties"), (20011, "plain"), (32768, "equal"), (32769, "plain")])
+def test_long_contexts_of_many_heads(n, kind):
+    """64 pairs: one selecting launch up to 32768 rows between sink and recent rows, several behind them."""
+    _run(1, 64, [n + 20], 301, kind=kind)
+
+
+@pytest.mark.parametrize("n_sink", [0, 1, 2, 3, 5])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_that_begin_anywhere_in_memory(n_sink, in_place):
+    """Weights of J at every offset from 16 bytes, with one to nine positions of them."""
+    _run(9, 3, [n_sink + 6 + i for i in range(1, 10)], 3, n_sink=n_sink, recent=6, in_place=in_place)
+    _run(3, 3, [n_sink + 6 + 1021, n_sink + 6 + 258, n_sink + 6 + 4], 100, n_sink=n_sink, recent=6, in_place=in_place, kind="ties")
+
+
 def test_many_rows_move_in_place():
     """Thousands of chunks over the rows of others: what is overwritten has been read."""
     _run(8, 8, [6000 - 17 * i for i in range(8)], 3500, recent=64, in_place=True, src="head")
