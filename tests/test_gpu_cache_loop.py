@@ -204,3 +204,61 @@ def test_a_step_as_a_captured_graph():
         finally:
             ctx.close()
     assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+@pytest.mark.parametrize("layout", ["head", "htd"])
+@pytest.mark.parametrize("mode", [0, 1])
+def test_next_to_slow_and_fast_steps_on_one_context(layout, mode):
+    """Slow, fast and ragged steps give the bits they give alone when the other operators run on their context (and workspace) in between."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    B, Hq, Hkv, rows, budget, recent = 3, 16, 4, 18000, 300, 64
+    c = ref.Cache(B, Hkv, rows, layout, page=64, seed=90)
+    small = ref.Cache(B, Hkv, 500, "head", seed=91)
+    g = torch.Generator().manual_seed(92)
+    q = torch.randn((B, Hq, 128), generator=g).to(torch.bfloat16).cuda()
+    lens, shared = i32([17900, 17000, 800]), i32([600, 601, 599])
+    rs = lens - recent
+    is_slow = torch.tensor([1, 0, 0], dtype=torch.uint8, device="cuda")
+    selector = None if mode == 0 else dict(gamma=1.0, beta=0.5, p=2.0, eta=0.1, lambda_clip=0.7, alpha_soft=0.5, alpha_cross=0.5, temp=1.0, eps=1e-8, nms_radius=8)
+    results = []
+    for between in (False, True):
+        ctx = c.context(Hq, n_sink=4, recent=recent, budget=budget, selector=selector)
+        ctx_small = small.context(Hq, n_sink=4, recent=recent, budget=budget)
+        try:
+            w = torch.zeros((B, Hkv, rows), device="cuda")
+            o = torch.zeros((B, Hq, 128), device="cuda")
+            kept, n_kept, left = torch.zeros((B, Hkv, budget), dtype=torch.int32, device="cuda"), torch.zeros((B, Hkv), dtype=torch.int32, device="cuda"), i32([0] * B)
+
+            def others():
+                if not between:
+                    return
+                sfi.sfi_weight_attn(ctx.handle, q, c.K, c.V, lens, 0, 1.0, w, w, o)
+                sfi.sfi_shared_attn(ctx.handle, q, c.K, c.V, lens, shared, 0, 601, 0, o)
+                sfi.sfi_evict(ctx.handle, c.K, c.V, lens, 0, budget, w, None, ctx_small.handle, small.K, small.V, left, None, None, None, kept, n_kept)
+                sfi.sfi_evict(ctx.handle, c.K, c.V, i32([900, 700, 800]), 1000, budget, w, None, ctx_small.handle, small.K, small.V, left, None, None, None, kept, n_kept)
+
+            seen = []
+            for _ in range(2):
+                out, idx, n = (torch.zeros((B, Hq, 128), device="cuda"), torch.zeros((B, Hkv, budget), dtype=torch.int32, device="cuda"),
+                               torch.zeros((B, Hkv), dtype=torch.int32, device="cuda"))
+                others()
+                sfi.sfi_slow_step(ctx.handle, q, c.K, c.V, lens, 0, budget, out, idx, n)
+                seen += [out.clone(), idx.clone(), n.clone()]
+                others()
+                sfi.sfi_fast_step(ctx.handle, q, c.K, c.V, idx, n, budget, rs, lens, out)
+                seen.append(out.clone())
+                others()
+                sfi.sfi_mixed_step(ctx.handle, q, c.K, c.V, is_slow, lens, rs, 0, budget, out, idx, n)
+                seen += [out.clone(), idx.clone(), n.clone()]
+                others()
+                sfi.sfi_dense_attn(ctx.handle, q, c.K, c.V, lens, 0, out)
+                seen.append(out.clone())
+            torch.cuda.synchronize()
+            assert sfi.sfi_device_status(ctx.handle) == 0
+            results.append(seen)
+        finally:
+            ctx.close()
+            ctx_small.close()
+    assert all(torch.equal(x, y) for x, y in zip(*results))
