@@ -1436,9 +1436,11 @@ void all_rows_view(const sfi_ctx* x, sfi_ctx* y) {
   y->cfg.selector_mode = 0;
   y->alpha = 1.0f;
 }
-// Splits of the shared rows (none where nothing can be shared): one workgroup per unit.  The sequences' own rows: three workgroups fit a unit and are shared
-// out where that is two per pair or more (32 sequences of 8 KV heads, 650 rows each: 27 us; four, five, eight per unit 33, 32, 33); below that one per
-// pair, which needs no records of its own (64 sequences, 33 to 512 rows: 27.5 us, two per pair 32, three 35).
+// Splits of the shared rows (none where nothing can be shared): one workgroup per unit.  The sequences' own rows: one workgroup per pair, which needs no
+// records of its own, or, with few pairs and more than three tiles to a wave, all tiles shared out to three workgroups per unit (as many as fit).
+// us, per pair / shared out: 48 pairs, 200, 400, 700, 1200 rows each 8.7 / 11.0, 12.0 / 11.0, 16.0 / 13.6, 22 / 14.4; 128 pairs 10.7 / 12.1, 14.5 / 15.1,
+// 18.8 / 19.7, 26.1 / 25.1, and 24.8 / 19.5 with 100 to 1201 rows; 192 pairs, 700 and 1200 rows 18.8 / 22.2, 27.2 / 30.2; 256 pairs 21 / 26.6, 29.6 / 38, 100 to
+// 1201 rows 28.4 / 28.2.  (Shared out to four to eight per unit: 32 to 33 us where three take 27.)
 void shared_splits(const sfi_ctx* x, SharedArgs* a) {
   const int cols = shared_cols(a->B * a->G), groups = (a->B * a->G + cols - 1) / cols;
   const int tiles = (a->max_shared + kTile - 1) / kTile;
@@ -1446,7 +1448,7 @@ void shared_splits(const sfi_ctx* x, SharedArgs* a) {
   a->n_shared = (int)std::min<int64_t>(std::min<int64_t>(units, kMaxSharedSplits), (tiles + kWaves - 1) / kWaves);
   const int wgs = 3 * x->n_cu / a->Hkv;
   const int own_tiles = (a->len_cap - a->max_shared + kTile - 1) / kTile + 1;
-  a->own_wgs = wgs >= 2 * a->B && a->B <= kMaxOwnPlan && own_tiles > kWaves ? std::min(wgs, a->B * ((own_tiles + kWaves - 1) / kWaves)) : 0;
+  a->own_wgs = wgs / 6 >= a->B && a->B <= kMaxOwnPlan && own_tiles > 3 * kWaves ? std::min(wgs, a->B * ((own_tiles + kWaves - 1) / kWaves)) : 0;
 }
 }  // namespace
 

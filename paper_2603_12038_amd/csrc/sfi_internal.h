@@ -265,7 +265,7 @@ struct MoveArgs {
 
 // Dense attention of a batch that shares its first rows.
 constexpr int kMaxSharedSplits = 40;  // records a query head has of the shared rows, of kSlotCap
-constexpr int kMaxOwnPlan = 384;  // sequences whose own rows can be shared out (two workgroups each, three per unit)
+constexpr int kMaxOwnPlan = 128;  // sequences whose own rows can be shared out (three workgroups per unit, six per pair)
 struct SharedArgs {
   const uint16_t* q;
   const uint16_t* K;

@@ -293,7 +293,7 @@ __device__ __forceinline__ void walk(Cols<NCB>& C, const Rows& R, int t0, int t1
     return;
   }
   // A loop in which every request is made, and the last tiles behind it: with a branch around requests the compiler waits for all that are on
-  // their way (32768 rows of 8 heads, 16 / 32 columns: 26.3 / 30.4 us, without the branch 25.1 / 29.8; paged, 65536 rows: 47 / 45 us, 6.0 TB/s).
+  // their way (16 columns, 8 heads, 32768 rows: 26.3 us, without the branch 25.1; 65536 rows, paged: 47 / 45 us, 6.0 TB/s).
   for (; t + (2 * DEPTH - 1) * NW < t1; t += DEPTH * NW) {
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) tile(d, t + d * NW, true);
@@ -427,13 +427,13 @@ __device__ __forceinline__ float* shared_record(const SharedArgs& a, int c, int 
   return c < a.B * a.G ? a.part + (((int64_t)(c / a.G) * a.Hq + h * a.G + c % a.G) * kSlotCap + split) * kPartStride : nullptr;
 }
 
-// The shared rows for few columns (16 NCB in all): a workgroup per KV head and split, every wave with rows of its own in registers.
-template <int NCB, bool PAGED>
+// The shared rows for few columns (16): a workgroup per KV head and split, every wave with rows of its own in registers.
+template <bool PAGED>
 __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const SharedArgs a) {
-  __shared__ __align__(16) float lds[join_floats<kWaves>(16 * NCB)];
+  __shared__ __align__(16) float lds[join_floats<kWaves>(16)];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, jg = lane >> 4, n = lane & 15;
   const int h = blockIdx.x, split = blockIdx.y;
-  Cols<NCB> C;
+  Cols<1> C;
   start(C);
   const Seen seen = load_columns(a, C, 0, h, jg, n);
   int bad = 0;
@@ -441,9 +441,9 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
     Rows R = rows_of(a, a.lead, h);
     R.hi = seen.most - 1;
     const int tiles = (seen.most + kTile - 1) / kTile;
-    walk<NCB, kWaves, 2, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, seen.least, wave, jg, n, a.scale_log2, bad);
+    walk<1, kWaves, 2, PAGED>(C, R, (int)((int64_t)tiles * split / a.n_shared), (int)((int64_t)tiles * (split + 1) / a.n_shared), 0, seen.least, wave, jg, n, a.scale_log2, bad);
   }
-  join<NCB, kWaves, true>(C, wave, 16 * NCB, 0, jg, n, lds, [&](int col) { return shared_record(a, col, h, split); });
+  join<1, kWaves, true>(C, wave, 16, 0, jg, n, lds, [&](int col) { return shared_record(a, col, h, split); });
   if (bad != 0 && a.guard != nullptr) atomicOr(a.guard, bad);
 }
 
@@ -457,9 +457,8 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
 //   weights' second terms, 1000 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200; the matrix pipe is busy 46 % of the time,
 //   the vector pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's products with V beside
 //   stage t + 1's weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.  32 sequences of
-//   32 heads over 16384 rows, paged (128 columns): 27 us for 67 MB: 12 us for the first rows and the records (17 MB), then 1.9 us for 64 rows of each
-//   split, of which two waves' 96 matrix instructions are 0.64.
-template <int NCB, int CG, int RG, bool THREE, bool PAGED>
+//   32 heads over 16384 rows, paged (two groups of 64 columns): 26 us for 67 MB, 8.6 GFLOP.
+template <bool PAGED, int NCB, int CG, int RG, bool THREE>
 __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
   constexpr int kLoads = kRowsHere * 16 / kThreads;  // of K, and as many of V, per thread and stage
@@ -581,8 +580,8 @@ constexpr int kOwnThreads = 64 * kOwnWaves;
 constexpr int kOwnAhead = 8;  // records a thread requests together
 constexpr int kDeviceScope = 16;  // cache-policy bit sc1 of the buffer instructions
 
-// Sequences that differ are evened out here rather than split alike: 100 to 1201 rows 32 us split alike, 30 shared out; all 650 27 both ways; one that shares
-// nothing among 31 that share 16384 rows is read by as many workgroups as it has records left, not by three.
+// Sequences that differ are evened out here rather than split alike (100 to 1201 rows: 32 us split alike, 30 shared out), and one that shares nothing among
+// others that share 16384 rows is read by as many workgroups as it has records left.
 // Which part of whose own rows workgroup `slot` of a KV head has, of own_wgs: tiles shared out evenly over the batch, as few to a workgroup as
 // the workgroups allow (at least one for each wave), every sequence at least one workgroup and at most as many as it has records.
 struct OwnShare {
@@ -641,9 +640,9 @@ __device__ __forceinline__ OwnShare own_share(const SharedArgs& a, int slot, int
   return {a.B, 0, 0};
 }
 
-// A sequence's own rows, one (ALONE) or several workgroups per KV head and sequence, and the merge.  Bound by the rows: 85 MB of 32 sequences (100 to 1201
-// rows of 8 KV heads, paged) in 30 us, 24 without the 17 MB of shared rows' records; 157 MB (1201 rows each) in 40 us, 4.4 TB/s with the records.
-// A tile per wave on its way: with two 48 us, as only two workgroups fit a unit then.  The last of a pair's workgroups to finish merges the
+// A sequence's own rows, one (ALONE) or several workgroups per KV head and sequence, and the merge.  Bound by the rows and the records: 32 sequences of
+// 8 KV heads with 1201 rows each 157 MB in 30 us, 5.3 TB/s; 100 to 1201 rows, paged, 85 MB and 9 MB of the shared rows' records, 28; one row each 8.
+// A tile per wave on its way: with two, two workgroups fit a unit in place of three, 40 -> 48 us.  The last of a pair's workgroups to finish merges the
 // records of all and those of the shared rows, which the launch before has left, into the output; records go from workgroup to workgroup at
 // device scope (stores and loads that name it, a count once the stores have been performed; the counter is zero between launches).
 // A pair with one workgroup keeps its record in LDS, and requests the shared rows' records before its waves are joined.
@@ -803,32 +802,27 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
 
 #define SFI_LAUNCH_PAGED(kernel, grid, threads, ...)                                                                        \
   do {                                                                                                                      \
-    if (a.table != nullptr) hipLaunchKernelGGL((kernel<__VA_ARGS__, true>), grid, dim3(threads), 0, s, a);                  \
-    else hipLaunchKernelGGL((kernel<__VA_ARGS__, false>), grid, dim3(threads), 0, s, a);                                    \
+    if (a.table != nullptr) hipLaunchKernelGGL((kernel<true __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(threads), 0, s, a);    \
+    else hipLaunchKernelGGL((kernel<false __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(threads), 0, s, a);                      \
   } while (0)
 
 constexpr int kTwoTermRows = 24576;
-int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 32 ? 32 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256; }
+// Columns (us of the shared rows' launch, 8 KV heads, three weight terms up to 16384 rows):
+//   up to 16 in registers: 2048 rows 7.7, 16384 rows 15.9, 65536 rows 45 (the kernel for many columns with 64: 7.5, 16.2, 56);
+//   up to 256 by 64, which read the rows from the caches again: 32 columns 7.8 / 16.8 (32 in registers 9.4 / 18.8); 128 columns, 2048 / 16384 rows, 10.8 / 26.2
+//   (all 128 at once 14.9 / 28.6); 256 columns, 4096 / 16384 rows 16.5 / 34.8 (256 at once 20 / 34.8);
+//   above by 256: 512 columns, 16384 / 32768 rows 56 / 105 (by 64 62 / 130, by 128 56 / 107), though 4096 rows 26.7 (23.9).
+int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 256 ? 64 : 256; }
 
 hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
   const int cols = shared_cols(a.B * a.G);
   const dim3 grid(a.Hkv, a.n_shared, (a.B * a.G + cols - 1) / cols);
   const bool three = a.out_bf16 == 0 && a.max_shared < kTwoTermRows;
-  switch (cols) {
-    case 16: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 1); break;
-    case 32: SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads, 2); break;
-    case 64:
-      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, true);
-      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, false);
-      break;
-    case 128:
-      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2, true);
-      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 4, 2, false);
-      break;
-    default:
-      if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, true);
-      else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, false);
-  }
+  if (cols == 16) SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads);
+  else if (cols == 64 && three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, true);
+  else if (cols == 64) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, false);
+  else if (three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, true);
+  else SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 2, 8, 1, false);
   return hipGetLastError();
 }
 hipError_t launch_own_rows(const SharedArgs& a, hipStream_t s) {
