@@ -233,7 +233,7 @@ struct RopeArgs {
 };
 
 // Eviction: the kept rows to the front of another cache, or of the same one.
-constexpr int kMoveRows = 64;    // rows per workgroup
+constexpr int kMoveRows = 64;    // rows per workgroup: four of K and four of V on their way in a thread
 struct MoveArgs {
   const uint16_t* K;
   const uint16_t* V;

