@@ -345,6 +345,8 @@ struct SelArgs {
   unsigned long long* met_out;  //   ... Workspace::met_out
   const uint32_t* wg_hist;  //   ... Workspace::wg_hist (mode 0)
   const double* wg_stat;   //   ... Workspace::wg_stat (full Selector)
+  int32_t place_x;         // the launch's segments lie along the grid's first index, not its second (set by the launch)
+  int32_t n_place;         //   ... how many of them it has
   // eviction and attention with running weights
   const float* weights;    // [B*Hkv][w_rows]
   float* w_out;            // the same shape
@@ -353,8 +355,6 @@ struct SelArgs {
   uint32_t* moved;         // Workspace::moved, cleared by the launch that reads the weights; nullptr: not
   int32_t moved_words;
   int32_t* guard;          // ... which reports a ctx_len that had to be clamped here
-  int32_t place_x;         // the launch's segments lie along the grid's first index, not its second (set by the launch)
-  int32_t n_place;         //   ... how many of them it has
 };
 
 // three_terms: logits exposed (no key norms), the weights in three terms

@@ -87,6 +87,9 @@ __device__ __forceinline__ uint4 load16(const char* p) {
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
+// A tile in registers.  A K row leaves as requests of 64 bytes, so the other half of a cache line comes from the L2 if it is left there: K through the caches, V (whole
+// lines at once) past them.  Own rows of 100 to 1201 and 300 rows 23.0 / 20.9 us (K past them too 27.4 / 23.0, V through them too 22.2 / 21.0), 1200 rows each
+// 29.7 (29.8, 36); 16 columns over 32768 / 65536 rows 23.5 / 44.9 (25.2 / 44.8, 23.4 / 50): rows that a case before has left in the last-level cache.
 struct Tile {
   uint4 ka[4], kb[4], v[8];
 };
@@ -96,8 +99,8 @@ __device__ __forceinline__ void issue_k(Tile& T, const Rows& R, const Block& A, 
   const char* pb = R.K + (uint64_t)(uint32_t)(min(max(r0 + 16 + n, B.first), B.last) + B.base) * R.k_st + jg * 16;
 #pragma unroll
   for (int kb = 0; kb < 4; ++kb) {
-    T.ka[kb] = load16<true>(pa + kb * 64);
-    T.kb[kb] = load16<true>(pb + kb * 64);
+    T.ka[kb] = load16<false>(pa + kb * 64);
+    T.kb[kb] = load16<false>(pb + kb * 64);
   }
 }
 template <bool PAGED>
