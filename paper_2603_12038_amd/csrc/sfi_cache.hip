@@ -12,7 +12,7 @@ namespace sfi {
 // A wave has one new row at a time (a token): lane i computes the sine and cosine of pair i once, through LDS they go to the lanes
 // that need them, and the row's heads (query, key, value) follow four at a time, 16 lanes of 16 bytes to a head.
 // Bound by the rows read and written: a prompt of 8192 rows of 48 heads, 201 MB in 36.5 us; 16 prompts of 700 to 2011 rows of 56 heads into a paged
-// cache, 622 MB in 130 us, 4.8 TB/s (a large copy reaches 5.1); four rows 4.1 us, a launch and three round trips.
+// cache, 622 MB in 130 us, 4.8 TB/s (a large copy reaches 5.1); four rows 4.0 us, a launch and three round trips.
 __global__ void rope_table_kernel(const RopeTable t, uint64_t* table) {
   if (threadIdx.x < kHeadDim / 2) table[threadIdx.x] = t.turn[threadIdx.x];
 }
@@ -33,7 +33,25 @@ __device__ __forceinline__ uint32_t bf16_any(float v) {
   return v != v ? 0x7fc0u | (__float_as_uint(v) >> 31 << 15) : bf16_rne(v);
 }
 
-// AHEAD: groups of four heads a wave requests together; one where it has no more than a few.
+// AHEAD groups of four heads of a new row (heads behind the last one repeat it), `there` or not.
+struct NewRow {
+  const uint16_t *q, *k, *v;
+  int Hq, Hkv;
+};
+template <int AHEAD>
+__device__ __forceinline__ void request_heads(u32x4 (&x)[AHEAD], const NewRow w, int h0, int step, int sub, int c, bool there) {
+#pragma unroll
+  for (int r = 0; r < AHEAD; ++r) {
+    const int h = min(h0 + r * step + sub, w.Hq + 2 * w.Hkv - 1);
+    const bool is_q = h < w.Hq, is_k = !is_q && h < w.Hq + w.Hkv;
+    const int hk = is_q ? h : is_k ? h - w.Hq : h - w.Hq - w.Hkv;
+    x[r] = u32x4{0u, 0u, 0u, 0u};
+    if (there) x[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((is_q ? w.q : is_k ? w.k : w.v) + hk * kHeadDim + 8 * c));
+  }
+}
+
+// AHEAD: groups of four heads a wave requests together; one where it has no more than a few.  Then the first
+// are on their way while sines are made (four rows 4.25 -> 4.0 us; with four groups a prompt of 8192 rows 36.7 -> 38.5).
 template <int AHEAD>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArgs a) {
   __shared__ float2 s_cs[kRopeWaves][kHeadDim / 2];  // cosine, sine
@@ -41,6 +59,10 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
   const int64_t token = (int64_t)blockIdx.x * kRopeWaves + wave;
   const int64_t n_tokens = (int64_t)a.B * a.max_new;
   const int b = (int)((token < n_tokens ? token : n_tokens - 1) / a.max_new), t = (int)((token < n_tokens ? token : n_tokens - 1) % a.max_new);
+  const int c = lane & 15, sub = lane >> 4;  // elements 8 c .. 8 c + 7 of head sub of each four
+  const NewRow in = {a.q + (int64_t)b * a.q_in_b + (int64_t)t * a.q_in_t, a.k + (int64_t)b * a.k_in_b + (int64_t)t * a.k_in_t,
+                     a.v + (int64_t)b * a.v_in_b + (int64_t)t * a.v_in_t, a.Hq, a.Hkv};
+  const int heads = a.Hq + 2 * a.Hkv, step = 4 * (int)gridDim.y;
   int bad = 0;
   const int L0 = a.ctx_len[b];
   const int L = min(max(L0, 0), a.len_cap);
@@ -57,6 +79,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
   }
   const int row = L - n + t;
   const bool live = token < n_tokens && t < n;
+  u32x4 x[AHEAD];
+  if (AHEAD == 1) request_heads<AHEAD>(x, in, 4 * (int)blockIdx.y, step, sub, c, live);
   const int64_t pos = a.pos != nullptr ? (int64_t)a.pos[b] + t : (int64_t)row;
   const int half = a.rot / 2;
   {
@@ -68,7 +92,6 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
     s_cs[wave][lane] = make_float2(cs * a.magnitude, sn * a.magnitude);
   }
   __syncthreads();
-  const int c = lane & 15, sub = lane >> 4;  // elements 8 c .. 8 c + 7 of head sub of each four
   // Half layout: element e < half goes with e + half; the partner's chunk is half / 8 lanes away.  Interleaved: 2 i with 2 i + 1.
   const bool turned = 8 * c < a.rot, upper = !a.interleaved && 8 * c >= half;
   const int partner = upper ? lane - half / 8 : lane + half / 8;
@@ -93,24 +116,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
     k_row = (int64_t)b * a.k_sb + (int64_t)row * a.k_st;
     v_row = (int64_t)b * a.v_sb + (int64_t)row * a.v_st;
   }
-  const uint16_t* q_in = a.q + (int64_t)b * a.q_in_b + (int64_t)t * a.q_in_t;
-  const uint16_t* k_in = a.k + (int64_t)b * a.k_in_b + (int64_t)t * a.k_in_t;
-  const uint16_t* v_in = a.v + (int64_t)b * a.v_in_b + (int64_t)t * a.v_in_t;
   uint16_t* q_out = a.q_out + ((int64_t)b * a.max_new + t) * a.Hq * kHeadDim;
-  const int heads = a.Hq + 2 * a.Hkv;
-  for (int h0 = 4 * blockIdx.y; h0 < heads; h0 += 4 * AHEAD * gridDim.y) {
-    u32x4 x[AHEAD];
-#pragma unroll
-    for (int r = 0; r < AHEAD; ++r) {  // (heads behind the last one repeat it)
-      const int h = min(h0 + 4 * r * (int)gridDim.y + sub, heads - 1);
-      const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
-      const int hk = is_q ? h : is_k ? h - a.Hq : h - a.Hq - a.Hkv;
-      x[r] = u32x4{0u, 0u, 0u, 0u};
-      if (live) x[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((is_q ? q_in : is_k ? k_in : v_in) + hk * kHeadDim + 8 * c));
-    }
+  for (int h0 = 4 * (int)blockIdx.y; h0 < heads; h0 += AHEAD * step) {
+    if (AHEAD > 1 || h0 != 4 * (int)blockIdx.y) request_heads<AHEAD>(x, in, h0, step, sub, c, live);
 #pragma unroll
     for (int r = 0; r < AHEAD; ++r) {
-      const int h = h0 + 4 * r * (int)gridDim.y + sub;
+      const int h = h0 + r * step + sub;
       const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + a.Hkv;
       const int hk = is_q ? h : is_k ? h - a.Hq : h - a.Hq - a.Hkv;
       const u32x4 w = x[r];
@@ -143,7 +154,7 @@ hipError_t launch_rope_append(const RopeArgs& a, int n_cu, hipStream_t s) {
   const int quads = (a.Hq + 2 * a.Hkv + 3) / 4;
   const unsigned gx = (unsigned)((tokens + kRopeWaves - 1) / kRopeWaves);
   // Heads split over workgroups until every unit has eight.  8192 rows of 48 heads, one group of heads at a time / four: 44 / 36.5 us (201 MB, 5.5 TB/s);
-  // four rows, a group each: 4.3 / 5.8.
+  // four rows, a group each: 4.0 / 5.8.
   int parts = (int)((8 * (int64_t)n_cu + gx - 1) / gx);
   if (parts > quads) parts = quads;
   if (parts < 1) parts = 1;
