@@ -138,7 +138,7 @@ size_t sfi_workspace_bytes(const sfi_config* cfg);
 
 /* Validate cfg, bind the caller's workspace, return a context in *out.
  * Touches the device to read its properties and to clear what the kernels expect to be zero between two calls: the
- * arrival counters of the fast step's in-kernel merge (512 bytes per sequence and KV head), for contexts whose slow step can
+ * arrival counters of the in-kernel merges (fast step, sfi_shared_attn: 512 bytes per sequence and KV head), for contexts whose slow step can
  * score in its dense launch (sfi_set_dense_scores) the statistics handed over there (512 bytes per sequence and query head), and the status word
  * of sfi_device_status.  A blocking memset followed by a device synchronisation, so not to be called while a stream of the device is
  * capturing.  SFI_ELAUNCH if the workspace is memory the runtime knows (device, managed or pinned host
@@ -422,7 +422,7 @@ int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_s
  *   shared_len  DEVICE int32 [B], brought into [0, min(ctx_len[b], ctx_len[lead], max_shared)] (SFI_GUARD_SHARED); the lead's own entry may be
  *               anything in that range.
  *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
- * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with more than 32
+ * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with more than 16
  * queries of a KV head in the batch (B * G) and a bf16 output or max_shared >= 24576, the softmax weights of the shared rows to 2^-18 of themselves.  Rows that only other
  * sequences share may hold anything.  Rows of their own are shared out to the compute units where the batch has few (sequence, KV head) pairs; where it
  * has many, each is read by one workgroup, and a sequence with far more of them than the others has better a call of its own.  Row strides below 2^29.

@@ -3,7 +3,7 @@
 // For a KV head the B x G queries of the batch are columns of one matrix product against the shared rows, masked by how many of them
 // each sequence shares; the rows that a sequence has of its own are a product with its G queries alone.  Both are cut into splits that leave flash
 // records (running maximum, sum and accumulator, log2 domain: weights 2^(y - m), y = log2(e) * logit) in the layout of the dense kernel,
-// [query head][split], and the merge launch joins them.
+// [query head][split], and the own rows' launch, the second of two, joins them.
 //
 // Matrix instructions (16x16x32 bf16, fp32 accumulation), a tile of 32 rows, blocks A and B of 16:
 //   S   = K (16 rows x 128) Q^T (128 x 16 columns): lane (jg = lane / 16, n = lane % 16) has logits of column n, rows 4 jg + i of a block
@@ -15,7 +15,7 @@
 // Three hold all 24 bits; two lose up to 2^-18, 2.4e-6 of the outputs' norm at any length where the weights are alike.  Two are taken for many columns where
 // the third is not seen: behind it a bf16 output rounds by 2^-9, and from kTwoTermRows shared rows on an fp32 sum in row order loses as much (3e-7 at
 // 200 rows, 1.2e-6 at 16384, 2.2e-6 at 32768; with three terms here 2e-7, 3e-7, 4e-7).  Time with two / three terms: 64 sequences of 64 heads over
-// 32768 rows 103 / 126 us, over 2048 18.8 / 20.1; 32 of 32 over 16384 28.3 / 30.
+// 32768 rows 103 / 126 us, over 2048 18.8 / 20.1; 16 of 32 over 16384 17.4 / 18.4.
 #include "sfi_internal.h"
 #include "sfi_wave.h"
 
