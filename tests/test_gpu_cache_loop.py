@@ -262,3 +262,94 @@ def test_next_to_slow_and_fast_steps_on_one_context(layout, mode):
             ctx.close()
             ctx_small.close()
     assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+@pytest.mark.parametrize("bad_id", [-1, 1 << 30])
+@pytest.mark.parametrize("B, Hq, Hkv", [(3, 4, 2), (3, 24, 2), (20, 32, 2)])
+def test_block_ids_outside_the_pool(B, Hq, Hkv, bad_id):
+    """One sequence's table names blocks that are not there: reported, the other sequences as they were, nothing written outside their rows."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    rows, budget, recent = 500, 60, 16
+    g = torch.Generator().manual_seed(95)
+    c, small = ref.Cache(B, Hkv, rows, "htd", page=16, seed=94), ref.Cache(B, Hkv, 120, "thd", page=16, seed=96)
+    ctx, ctx_small = c.context(Hq, n_sink=4, recent=recent, budget=budget), small.context(Hq, n_sink=0, recent=0, budget=0)
+    q = torch.randn((B, Hq, 128), generator=g).to(torch.bfloat16).cuda()
+    w0 = torch.rand((B, Hkv, rows), generator=g).cuda()
+    lens, shared = i32([480 - 7 * b for b in range(B)]), i32([200] * B)
+    good, good_small, empty = c.table.clone(), small.table.clone(), [t.clone() for t in small.store]
+    others = [b for b in range(B) if b != 1]
+
+    def call(bad, bad_small):
+        c.table.copy_(good)
+        small.table.copy_(good_small)
+        for t, e in zip(small.store, empty):
+            t.copy_(e)
+        if bad:
+            c.table[1, 13:20] = bad_id
+        if bad_small:
+            small.table[1, 2:4] = bad_id
+        a, d, w = torch.zeros((B, Hq, 128), device="cuda"), torch.zeros((B, Hq, 128), device="cuda"), torch.zeros((B, Hkv, rows), device="cuda")
+        kept, n_kept, left = torch.zeros((B, Hkv, budget), dtype=torch.int32, device="cuda"), torch.zeros((B, Hkv), dtype=torch.int32, device="cuda"), i32([0] * B)
+        seen = []
+        for name in ("shared", "weigh", "evict"):
+            _step(f"B={B} heads {Hq}/{Hkv} {name} bad={bad, bad_small, bad_id}")
+            if name == "shared":
+                sfi.sfi_shared_attn(ctx.handle, q, c.K, c.V, lens, shared, 0, 200, 0, a)
+            elif name == "weigh":
+                sfi.sfi_weight_attn(ctx.handle, q, c.K, c.V, lens, 0, 1.0, w0, w, d)
+            else:
+                sfi.sfi_evict(ctx.handle, c.K, c.V, lens, 0, budget, w0, None, ctx_small.handle, small.K, small.V, left, None, None, None, kept, n_kept)
+            torch.cuda.synchronize()
+            seen.append(sfi.sfi_device_status(ctx.handle))
+        return seen, a, d, w, kept, n_kept, left, [t.clone() for t in small.store]
+
+    try:
+        want = call(False, False)
+        assert want[0] == [0, 0, 0]
+        got = call(True, False)
+        assert got[0] == [8, 8, 8]
+        for x, y in zip(got[1:4], want[1:4]):
+            assert torch.equal(x[others], y[others])
+        assert all(torch.equal(x, y) for x, y in zip(got[4:7], want[4:7]))
+        mine = set(small.table_np[1].tolist())
+        rest = [i for i in range(small.n_blocks) if i not in mine]
+        for x, y in zip(got[7], want[7]):
+            assert torch.equal(x[rest], y[rest])
+        got = call(False, True)
+        assert got[0] == [0, 0, 8]
+        gone = small.table_np[1, 2:4].tolist()
+        for x, y, e in zip(got[7], want[7], empty):
+            keep = [i for i in range(small.n_blocks) if i not in gone]
+            assert torch.equal(x[keep], y[keep]) and torch.equal(x[gone], e[gone])
+    finally:
+        ctx.close()
+        ctx_small.close()
+
+
+@pytest.mark.parametrize("Hq", [4, 24])
+def test_a_leads_block_ids_outside_the_pool(Hq):
+    """Reported only where the rows are used: sequences that share none of them are as they were."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    B, Hkv, rows = 3, 2, 400
+    c = ref.Cache(B, Hkv, rows, "htd", page=16, seed=97)
+    ctx = c.context(Hq)
+    q = torch.randn((B, Hq, 128), generator=torch.Generator().manual_seed(98)).to(torch.bfloat16).cuda()
+    lens = i32([350, 340, 330])
+    try:
+        out = []
+        for shared, bad in (([192, 192, 0], False), ([192, 192, 0], True)):
+            if bad:
+                c.table[0, 3] = c.n_blocks
+            o = torch.zeros((B, Hq, 128), device="cuda")
+            _step(f"lead, heads {Hq}/{Hkv} bad={bad}")
+            sfi.sfi_shared_attn(ctx.handle, q, c.K, c.V, lens, i32(shared), 0, 192, 0, o)
+            torch.cuda.synchronize()
+            assert sfi.sfi_device_status(ctx.handle) == (8 if bad else 0)
+            out.append(o)
+        assert torch.equal(out[0][2], out[1][2]) and out[1].isfinite().all()
+    finally:
+        ctx.close()
