@@ -795,9 +795,8 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     const Share r = share_of(g0);  // the threads that stored before
     if (r.rl != 0) continue;
     const float4 v = *reinterpret_cast<const float4*>(&s_own[r.g][4 + 4 * r.c]);
-    const float z = s_own[r.g][1];
-    store_out4(a.out, (head0 + r.g) * kHeadDim + 4 * r.c, z > 0.f ? make_float4(v.x / z, v.y / z, v.z / z, v.w / z) : make_float4(0.f, 0.f, 0.f, 0.f),
-               a.out_bf16 != 0);
+    const float z = s_own[r.g][1], f = z == 0.f ? 0.f : 1.0f / z;  // no row: 0; a NaN that was seen is in z or v, and stays
+    store_out4(a.out, (head0 + r.g) * kHeadDim + 4 * r.c, make_float4(v.x * f, v.y * f, v.z * f, v.w * f), a.out_bf16 != 0);
   }
 }
 
