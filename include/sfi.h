@@ -407,7 +407,8 @@ int sfi_set_rope(sfi_ctx* ctx, const sfi_rope* rope, void* stream);
  *   q_out    bf16 [B, max_new, Hq, 128] contiguous; may be q itself where that is laid out alike, and may not overlap q otherwise.
  *   K, V     the cache as in the hot calls, written here.  n_new, pos: DEVICE int32 [B].
  * Padding (t >= n_new[b]) is not read, and q_out keeps what it holds there.  A row whose block id is out of range is not written.
- * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW).  Needs sfi_set_rope.  B * max_new up to 2^26 - 4.
+ * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW); with n_new NULL an unused slot (ctx_len[b] = 0) gets no rows, and no flag
+ * is set for it.  Needs sfi_set_rope.  B * max_new up to 2^26 - 4.
  */
 int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* k, int64_t k_stride_b, int64_t k_stride_t,
                     const void* v, int64_t v_stride_b, int64_t v_stride_t, const int32_t* ctx_len, const int32_t* n_new, const int32_t* pos,
@@ -568,7 +569,7 @@ int sfi_plan_splits(const sfi_ctx* ctx, int32_t max_len, int32_t sel_stride, int
 #define SFI_GUARD_N_SEL 2   /* an n_sel[b, h] was negative or above sel_stride */
 #define SFI_GUARD_SEL_IDX 4 /* an index among sel_idx[b, h, 0:n_sel] was outside [0, ctx_len[b]) */
 #define SFI_GUARD_BLOCK 8   /* a block-table entry covering rows [0, ctx_len[b]) was outside [0, n_blocks) */
-#define SFI_GUARD_N_NEW 16  /* an n_new[b] was negative or above max_new or ctx_len[b] */
+#define SFI_GUARD_N_NEW 16  /* an n_new[b] was negative or above max_new or ctx_len[b], or max_new (n_new NULL) was above a ctx_len[b] > 0 */
 #define SFI_GUARD_SHARED 32 /* a shared_len[b] was negative or above max_shared, ctx_len[b] or ctx_len[lead] */
 int sfi_device_status(sfi_ctx* ctx, int32_t* flags, int32_t clear, void* stream);
 

@@ -74,8 +74,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(const RopeArg
     bad |= n != n0 ? kGuardNNew : 0;
   }
   if (n > L) {
+    bad |= a.n_new != nullptr || L > 0 ? kGuardNNew : 0;  // (max_new for every sequence: none for an unused slot)
     n = L;
-    bad |= kGuardNNew;
   }
   const int row = L - n + t;
   const bool live = token < n_tokens && t < n;

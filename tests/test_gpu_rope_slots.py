@@ -1,0 +1,42 @@
+"""sfi_rope_append for a batch with unused slots, and queries that are written where they are read."""
+import numpy as np
+import pytest
+
+import cache_ref as ref
+from cache_ref import bits, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("layout", ["head", "thd"])
+@pytest.mark.parametrize("new", [1, 5])
+def test_unused_slots_take_no_rows_and_raise_no_flag(layout, new):
+    """ctx_len 0 with every sequence getting `new` rows: nothing is written for the slot, and nothing is reported."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    lens = [20, 0, new, 0]
+    cache = ref.Cache(4, 2, 32, layout, seed=15)
+    ctx = cache.context(4)
+    try:
+        sfi.sfi_set_rope(ctx.handle, 64)
+        before = [cache.numpy(0), cache.numpy(1)]
+        g = torch.Generator().manual_seed(16)
+        q, k = (torch.randn((4, new, h, 128), generator=g).to(torch.bfloat16).cuda() for h in (4, 2))
+        q_out = torch.full_like(q, 7.0)
+        sfi.sfi_rope_append(ctx.handle, q, k, k, i32(lens), None, None, q_out, cache.K, cache.V)
+        torch.cuda.synchronize()
+        assert sfi.sfi_device_status(ctx.handle) == 0
+        after = [cache.numpy(0), cache.numpy(1)]
+        for b, n in enumerate(lens):
+            if n == 0:
+                assert (bits(q_out)[b] == bits(torch.tensor([7.0], dtype=torch.bfloat16))[0]).all()
+                assert all(np.array_equal(x[b], y[b]) for x, y in zip(after, before))
+            else:
+                assert np.array_equal(after[1][b, :, n - new:n].transpose(1, 0, 2), bits(k)[b])
+        # a length that is there but does not hold the new rows is still reported
+        sfi.sfi_rope_append(ctx.handle, None, k, k, i32([20, 0, max(new - 1, 1), 0]), None, None, None, cache.K, cache.V)
+        torch.cuda.synchronize()
+        assert sfi.sfi_device_status(ctx.handle) == (sfi.binding.GUARD_N_NEW if new > 1 else 0)
+    finally:
+        ctx.close()
