@@ -423,8 +423,8 @@ int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_s
  *   shared_len  DEVICE int32 [B], brought into [0, min(ctx_len[b], ctx_len[lead], max_shared)] (SFI_GUARD_SHARED); the lead's own entry may be
  *               anything in that range.
  *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
- * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with more than 16
- * queries of a KV head in the batch (B * G) and a bf16 output or max_shared >= 24576, the softmax weights of the shared rows to 2^-18 of themselves.  Rows that only other
+ * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with a bf16 output and
+ * more than 16 queries of a KV head in the batch (B * G), the softmax weights of the shared rows to 2^-17 of themselves.  Rows that only other
  * sequences share may hold anything.  Rows of their own are shared out to the compute units where the batch has few (sequence, KV head) pairs; where it
  * has many, each is read by one workgroup, and a sequence with far more of them than the others has better a call of its own.  Row strides below 2^29.
  */

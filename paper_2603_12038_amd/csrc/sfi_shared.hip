@@ -11,11 +11,11 @@
 //         4 jg + i - 4 of block B, where the first product left this lane's weights.  Product e of eight takes dim 8 m + e as its row m, so
 //         lane (jg, n) loads 16 bytes of a V row as they lie (dims 8 n .. + 7), and has dims 8 (4 jg + i) + e of column n in the end:
 //         maximum, sum and accumulator of a column stay in the lanes that have its logits.
-// A weight goes into the second product as the sum of bf16 terms, each to nearest: with one the output would carry the weights' 2^-9.
-// Three hold all 24 bits; two lose up to 2^-18, 2.4e-6 of the outputs' norm at any length where the weights are alike.  Two are taken for many columns where
-// the third is not seen: behind it a bf16 output rounds by 2^-9, and from kTwoTermRows shared rows on an fp32 sum in row order loses as much (3e-7 at
-// 200 rows, 1.2e-6 at 16384, 2.2e-6 at 32768; with three terms here 2e-7, 3e-7, 4e-7).  Time with two / three terms: 64 sequences of 64 heads over
-// 32768 rows 103 / 126 us, over 2048 18.8 / 20.1; 16 of 32 over 16384 17.4 / 18.4.
+// A weight goes into the second product as the sum of bf16 terms, each to nearest: with one the output would carry the weights' 2^-8.
+// Three hold all 24 bits; two lose up to 2^-17, 2.4e-6 of the outputs' norm where the weights are alike (three: 2e-7 at 200 rows, 3e-7 at 16384,
+// 4e-7 at 32768).  Two are taken for many columns behind a bf16 output alone, which rounds by up to 2^-8 itself: what an fp32 output holds does
+// not depend on how many columns or rows a launch has room for.  Time with two / three terms, one row of their own:
+// 64 sequences of 64 heads over 32768 rows 93 / 122 us, over 2048 17.2 / 18.4; 16 of 32 over 16384 15.6 / 16.1.
 #include "sfi_internal.h"
 #include "sfi_wave.h"
 
@@ -456,11 +456,11 @@ __global__ __launch_bounds__(kAttnThreads, 1) void shared_few_kernel(const Share
 //   stage.  In LDS the 16-byte pieces of K row r stand at piece ^ (r & 15), the 32-byte pieces of V row r at piece ^ (r & 7): what 16 lanes read
 //   together, one piece of 16 rows of K, or of 4 rows of V (transposed on the way: ds_read_b64_tr_b16 gives a lane one dim of
 //   four rows), lies in different banks.
-// - Eight waves, two on each SIMD.  64 sequences of 64 heads over 32768 rows of 8 KV heads: 100 to 106 us, 69.3 GFLOP and half as many again for the
-//   weights' second terms, 1000 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200; the matrix pipe is busy 46 % of the time,
-//   the vector pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's products with V beside
-//   stage t + 1's weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.  32 sequences of
-//   32 heads over 16384 rows, paged (two groups of 64 columns): 26 us for 67 MB, 8.6 GFLOP.
+// - Eight waves, two on each SIMD.  64 sequences of 64 heads over 32768 rows of 8 KV heads: three terms 122 us, 69.3 GFLOP and as many again for the second
+//   and third terms, 1140 TFLOP/s of matrix instructions where a library's 8192^3 product reaches 1200.  Two terms 93 to 106 us for 104 GFLOP; there
+//   the matrix pipe is busy 46 % of the time, the vector pipe as long, and other orders did not bring them closer together: waves of a SIMD in turn 111, stage t's
+//   products with V beside stage t + 1's weights and stage t + 2's products with K in steps of four 112, one wave per SIMD with 64 columns (spills) 214.
+//   32 sequences of 32 heads over 16384 rows, paged (two groups of 64 columns), two terms: 26 us for 67 MB, 8.6 GFLOP.
 template <bool PAGED, int NCB, int CG, int RG, bool THREE>
 __global__ __launch_bounds__(64 * CG * RG, 1) void shared_many_kernel(const SharedArgs a) {
   constexpr int kThreads = 64 * CG * RG, kRowsHere = kTile * RG, kCols = 16 * NCB * CG;
@@ -808,18 +808,17 @@ __global__ __launch_bounds__(kOwnThreads, 3) void own_rows_kernel(const SharedAr
     else hipLaunchKernelGGL((kernel<false __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(threads), 0, s, a);                      \
   } while (0)
 
-constexpr int kTwoTermRows = 24576;
-// Columns (us of the shared rows' launch, 8 KV heads, three weight terms up to 16384 rows):
-//   up to 16 in registers: 2048 rows 7.7, 16384 rows 15.9, 65536 rows 45 (the kernel for many columns with 64: 7.5, 16.2, 56);
+// Columns (us of the shared rows' launch, 8 KV heads, three weight terms where not said otherwise):
+//   up to 16 in registers: 2048 rows 7.7, 16384 rows 15.9, 65536 rows 45 (the kernel for many columns with 64: 7.5, 16.2, with two terms 56);
 //   up to 256 by 64, which read the rows from the caches again: 32 columns 7.8 / 16.8 (32 in registers 9.4 / 18.8); 128 columns, 2048 / 16384 rows, 10.8 / 26.2
 //   (all 128 at once 14.9 / 28.6); 256 columns, 4096 / 16384 rows 16.5 / 34.8 (256 at once 20 / 34.8);
-//   above by 256: 512 columns, 16384 / 32768 rows 56 / 105 (by 64 62 / 130, by 128 56 / 107), though 4096 rows 26.7 (23.9).
+//   above by 256: 512 columns, 16384 / 32768 rows 63 / 122 (by 64 69 / 145; two terms 51 / 93, by 64 59 / 114), though 4096 rows 24.8 (22.5).
 int shared_cols(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 256 ? 64 : 256; }
 
 hipError_t launch_shared_rows(const SharedArgs& a, hipStream_t s) {
   const int cols = shared_cols(a.B * a.G);
   const dim3 grid(a.Hkv, a.n_shared, (a.B * a.G + cols - 1) / cols);
-  const bool three = a.out_bf16 == 0 && a.max_shared < kTwoTermRows;
+  const bool three = a.out_bf16 == 0;
   if (cols == 16) SFI_LAUNCH_PAGED(shared_few_kernel, grid, kAttnThreads);
   else if (cols == 64 && three) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, true);
   else if (cols == 64) SFI_LAUNCH_PAGED(shared_many_kernel, grid, 512, 1, 4, 2, false);

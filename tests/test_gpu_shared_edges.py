@@ -57,3 +57,58 @@ def test_what_is_no_number_stays_none(B, Hq, Hkv, layout, own, bf16):
             assert (np.abs(got[b] - want) <= bound)[~bad].all(), b
     finally:
         ctx.close()
+
+
+def _two_terms_miss():
+    """Query values x > 0 in bf16 whose weight 2^(-x log2(e) / sqrt(128)), beside one of 1, is off by at least 2^-18 of itself as the sum of two bf16 terms."""
+    import torch
+
+    x = torch.arange(1, 2048, dtype=torch.float32).mul_(2.0 ** -5).to(torch.bfloat16).unique().double()
+    p = torch.exp(-x / 128.0 ** 0.5).float()
+    hi = p.to(torch.bfloat16).float()
+    lo = (p - hi).to(torch.bfloat16).float()
+    return x[(((p - hi - lo).abs() / p) >= 2.0 ** -18) & (p > 0.02)]
+
+
+def test_values_that_tell_two_terms_from_three():
+    """(of the check below: it has values to work with)"""
+    assert len(_two_terms_miss()) >= 16
+
+
+# Half of the rows have a weight of 1 and values of 0, the others a weight p and values of 1: the output is p / (1 + p), and its error that of p
+# in the products with V (the sums of the weights are in fp32).  In fp32 p is off by its exponent's two roundings (together below 7 2^-24: |exponent| < 6, times ln 2) and
+# 2^-23 for the exponential; the sums of either side round a few times per tile, wave and record.  That is below 48 roundings of at most 2^-24, to either side:
+# 2^-24 sqrt(48 / 3) = 2^-22 as a root of the mean square over columns of many p.  Two bf16 terms are off by 2^-18 or more in every column, and so is the
+# output: 2^-20 lies between.
+EXACT = 2.0 ** -20
+
+
+@pytest.mark.parametrize("B, Hq, Hkv", [(2, 8, 1), (5, 16, 4), (6, 32, 2), (20, 16, 1), (17, 64, 4)])
+@pytest.mark.parametrize("max_shared", [512, 24575, 24576, 30000])
+@pytest.mark.parametrize("own", [0, 96])
+def test_weights_keep_their_bits_behind_fp32_outputs(B, Hq, Hkv, max_shared, own):
+    """8 to 320 columns a head, the bound of the shared rows exact and far too large: the same accuracy."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    n, rows = 512, max_shared + own + 8
+    xs = _two_terms_miss()
+    K = torch.zeros((1, 1, rows, 128), dtype=torch.bfloat16)
+    V = torch.zeros((1, 1, rows, 128), dtype=torch.bfloat16)
+    K[:, :, 1::2, 0], V[:, :, 1::2] = 1.0, 1.0
+    K, V = (t.cuda().expand(B, Hkv, rows, 128) for t in (K, V))  # strides of zero: all sequences hold the same rows
+    ctx = sfi.SfiContext(B, Hq, Hkv, rows, 64, 4, 64, K, V)
+    try:
+        x = xs[torch.arange(B * Hq) * 7919 % len(xs)].view(B, Hq)
+        q = torch.zeros((B, Hq, 128), dtype=torch.bfloat16)
+        q[:, :, 0] = -x.to(torch.bfloat16)
+        q, out = q.cuda(), torch.zeros((B, Hq, 128), device="cuda")
+        _step(f"B={B} heads {Hq}/{Hkv} bound {max_shared} own {own}")
+        sfi.sfi_shared_attn(ctx.handle, q, K, V, i32([n + own] * B), i32([n] * B), 0, max_shared, 0, out)
+        torch.cuda.synchronize()
+        p = torch.exp(-x / 128.0 ** 0.5)
+        want = (p / (1 + p))[:, :, None]
+        off = out.cpu().double() / want - 1
+        assert off.square().mean().sqrt().item() <= EXACT
+    finally:
+        ctx.close()
