@@ -50,6 +50,7 @@ class SfiRope(C.Structure):
 
 _lib: Optional[C.CDLL] = None
 _hot = None  # the CPython module with the hot calls
+_heads = {}  # sequences, query heads and KV heads of each context made by sfi_create here, by handle
 
 EXPORTS = ("sfi_workspace_bytes", "sfi_create", "sfi_set_block_table", "sfi_destroy", "sfi_strerror", "sfi_slow_step", "sfi_slow_attn",
            "sfi_slow_select", "sfi_evidence_add", "sfi_evidence_add_causal", "sfi_evidence_select", "sfi_dense_attn",
@@ -203,6 +204,7 @@ def sfi_create(cfg: SfiConfig, workspace, workspace_bytes: int) -> int:
     """Returns the opaque context handle (an integer address); raises SfiError on a bad configuration."""
     h = C.c_void_p()
     _check(load_library().sfi_create(C.byref(cfg), _ptr(workspace), workspace_bytes, C.byref(h)), "sfi_create")
+    _heads[h.value] = cfg.batch, cfg.n_q_heads, cfg.n_kv_heads
     return h.value
 
 
@@ -214,6 +216,7 @@ def sfi_set_block_table(ctx, block_table, n_blocks: int) -> None:
 
 def sfi_destroy(ctx: int) -> None:
     _check(load_library().sfi_destroy(ctx), "sfi_destroy")
+    _heads.pop(getattr(ctx, "value", ctx), None)
 
 
 def sfi_slow_step(ctx, q, K, V, ctx_len, max_len, budget, out, sel_idx, n_sel, stream=None) -> None:
@@ -350,14 +353,36 @@ def sfi_set_rope(ctx, rot_dim: int, base: float = 10000.0, interleaved: bool = F
     _check(load_library().sfi_set_rope(ctx, C.byref(r), _stream(stream)), "sfi_set_rope")
 
 
+def _not_rows(name: str, x, want):
+    return AssertionError(f"{name}: rows {list(want)} with the heads of a row contiguous are wanted, got {list(x.shape)} with strides {list(x.stride())}")
+
+
 def sfi_rope_append(ctx, q, k, v, ctx_len, n_new, pos, q_out, K, V, stream=None) -> None:
     """q: bf16 tensor [B, new, Hq, 128], k, v: [B, new, Hkv, 128], the heads of a row contiguous (views of one projection's output will do);
-    q and q_out (contiguous) may be None together.  n_new, pos: int32 [B] or None."""
-    qs, ks, vs = (0, 0, 128, 1) if q is None else q.stride(), k.stride(), v.stride()
-    _, new, heads, d = k.shape
-    assert qs[3] == ks[3] == vs[3] == 1 and (heads == 1 or ks[2] == vs[2] == d) and (qs[2] == d or q.shape[2] == 1) and v.shape == k.shape
-    assert q is None or (q.shape[1] == new and q_out.is_contiguous())
-    (_hot or _load_hot()).sfi_rope_append(ctx, q, qs[0], qs[1], k, ks[0], ks[1], v, vs[0], vs[1], ctx_len, n_new, pos, new, q_out, K, V, stream)
+    q and q_out (contiguous) may be None together.  n_new, pos: int32 [B] or None.  AssertionError: a tensor of another shape."""
+    shape = k.shape
+    B, Hq, Hkv = _heads.get(ctx if type(ctx) is int else getattr(ctx, "value", None)) or (shape[0], None if q is None else q.shape[2], shape[2])
+    new = shape[1]
+    want = (B, new, Hkv, 128)
+    k_b, k_t, k_h, k_e = k.stride() if shape == want else (0, 0, 0, 0)
+    if k_e != 1 or (k_h != 128 and Hkv != 1):
+        raise _not_rows("k", k, want)
+    v_b, v_t, v_h, v_e = v.stride() if v.shape == want else (0, 0, 0, 0)
+    if v_e != 1 or (v_h != 128 and Hkv != 1):
+        raise _not_rows("v", v, want)
+    q_b = q_t = 0
+    if q is not None:
+        want = (B, new, Hq, 128)
+        q_b, q_t, q_h, q_e = q.stride() if q.shape == want else (0, 0, 0, 0)
+        if q_e != 1 or (q_h != 128 and Hq != 1):
+            raise _not_rows("q", q, want)
+        if q_out is not None and not (q_out.is_contiguous() and q_out.shape == want):
+            raise _not_rows("q_out (contiguous)", q_out, want)
+    if new == 1:  # the stride of a dimension of one is never used, and may be anything
+        q_t = k_t = v_t = 0
+    if B == 1:
+        q_b = k_b = v_b = 0
+    (_hot or _load_hot()).sfi_rope_append(ctx, q, q_b, q_t, k, k_b, k_t, v, v_b, v_t, ctx_len, n_new, pos, new, q_out, K, V, stream)
 
 
 def sfi_shared_attn(ctx, q, K, V, ctx_len, shared_len, lead: int, max_shared: int, max_len: int, out, stream=None) -> None:

@@ -40,3 +40,25 @@ def test_unused_slots_take_no_rows_and_raise_no_flag(layout, new):
         assert sfi.sfi_device_status(ctx.handle) == (sfi.binding.GUARD_N_NEW if new > 1 else 0)
     finally:
         ctx.close()
+
+
+def test_a_dimension_of_one_may_have_any_stride():
+    """One new row per sequence out of a tensor whose row stride is odd: the same bits as from a contiguous one."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    caches = [ref.Cache(3, 2, 32, "head", seed=17) for _ in range(2)]
+    got = []
+    for cache, stride in zip(caches, (512, 5)):
+        ctx = cache.context(4)
+        try:
+            sfi.sfi_set_rope(ctx.handle, 128)
+            g = torch.Generator().manual_seed(18)
+            q, k = (torch.randn(3 * h * 128, generator=g).to(torch.bfloat16).cuda().as_strided((3, 1, h, 128), (h * 128, stride, 128, 1)) for h in (4, 2))
+            q_out = torch.zeros((3, 1, 4, 128), dtype=torch.bfloat16, device="cuda")
+            sfi.sfi_rope_append(ctx.handle, q, k, k, i32([9, 1, 32]), None, None, q_out, cache.K, cache.V)
+            torch.cuda.synchronize()
+            got.append([bits(q_out), cache.numpy(0), cache.numpy(1)])
+        finally:
+            ctx.close()
+    assert all(np.array_equal(a, b) for a, b in zip(*got))
