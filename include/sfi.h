@@ -404,7 +404,7 @@ int sfi_set_rope(sfi_ctx* ctx, const sfi_rope* rope, void* stream);
  * the number of its cache row (the two part where rows have been evicted).
  *   q        bf16, head g of new row t of sequence b at q + b * q_stride_b + t * q_stride_t + g * 128 (strides in elements, multiples of 8: the
  *            three may be parts of one projection's output); k, v the same with n_kv_heads heads.  q may be NULL (with q_out).
- *   q_out    bf16 [B, max_new, Hq, 128] contiguous; may be q itself where that is laid out alike, and may not overlap q otherwise.
+ *   q_out    bf16 [B, max_new, Hq, 128] contiguous; may be q itself where that is laid out alike (SFI_EINVAL where not), and may not overlap q otherwise.
  *   K, V     the cache as in the hot calls, written here.  n_new, pos: DEVICE int32 [B].
  * Padding (t >= n_new[b]) is not read, and q_out keeps what it holds there.  A row whose block id is out of range is not written.
  * n_new[b] is brought into [0, min(max_new, ctx_len[b])] (SFI_GUARD_N_NEW); with n_new NULL an unused slot (ctx_len[b] = 0) gets no rows, and no flag

@@ -1491,6 +1491,9 @@ int sfi_rope_append(sfi_ctx* x, const void* q, int64_t q_stride_b, int64_t q_str
       misaligned(ctx_len, 4) || misaligned(n_new, 4) || misaligned(pos, 4))
     return SFI_EALIGN;
   const sfi_config& c = x->cfg;
+  const int64_t q_row = (int64_t)c.n_q_heads * kHeadDim;
+  if (q != nullptr && q_out == q && ((max_new > 1 && q_stride_t != q_row) || (c.batch > 1 && q_stride_b != max_new * q_row)))
+    return SFI_EINVAL;  // in place, laid out otherwise: rows would be written that others have yet to read
   CallRecord call_record(x);
   RopeArgs a;
   memset(&a, 0, sizeof(a));

@@ -62,3 +62,19 @@ def test_a_dimension_of_one_may_have_any_stride():
         finally:
             ctx.close()
     assert all(np.array_equal(a, b) for a, b in zip(*got))
+
+
+def test_queries_in_place_have_to_be_laid_out_like_the_output():
+    """Refused on the host, before anything is launched: q_out at q, whose rows lie further apart than the output's."""
+    import paper_2603_12038_amd as sfi
+
+    cache = ref.Cache(2, 2, 16, "head", seed=19)
+    ctx = cache.context(4)
+    try:
+        sfi.sfi_set_rope(ctx.handle, 128)
+        p = cache.K.data_ptr()
+        for new, qb, qt in ((1, 1024, 512), (3, 3 * 512, 1024), (3, 3 * 1024, 1024), (3, 512, 3 * 512)):
+            a = dict(q=p, qb=qb, qt=qt, k=p, kb=256, kt=256, v=p, vb=256, vt=256, ctx_len=p, n_new=p, pos=p, max_new=new, q_out=p, K=p, V=p)
+            assert sfi.load_library().sfi_rope_append(ctx.handle, *a.values(), None) == -1, (new, qb, qt)
+    finally:
+        ctx.close()
