@@ -4,6 +4,7 @@ import pytest
 
 import cache_ref as ref
 from cache_ref import bits, i32, to64
+from test_gpu_shared_attn import _run
 
 pytestmark = pytest.mark.gpu
 
@@ -110,5 +111,65 @@ def test_weights_keep_their_bits_behind_fp32_outputs(B, Hq, Hkv, max_shared, own
         want = (p / (1 + p))[:, :, None]
         off = out.cpu().double() / want - 1
         assert off.square().mean().sqrt().item() <= EXACT
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("layout", ["head", "token", "htd"])
+@pytest.mark.parametrize("B, Hq, Hkv", [(17, 16, 1), (33, 32, 2), (41, 28, 4)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_more_than_256_columns(B, Hq, Hkv, layout, bf16):
+    """272, 528 and 287 columns a head: the last group of 256 partly empty, shares of every length, tiles and stages cut anywhere."""
+    n = 1100
+    shared = [n - (i * 389) % (n + 1) for i in range(B)]
+    shared[B // 2] = 0
+    _run(B, Hq, Hkv, [max(s, 1) + (i * 53) % 70 for i, s in enumerate(shared)], shared, layout=layout, bf16=bf16, page=32)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B", [2, 17])
+def test_bounds_far_above_the_lengths(B, bf16):
+    """17 columns and more under a bound of max_ctx: the rows that are there decide, not the bound."""
+    _run(B, 16, 1, [90 + i for i in range(B)], [90 - i for i in range(B)], max_shared=90 + B + 39 - 1, bf16=bf16)
+
+
+@pytest.mark.parametrize("layout", ["head", "htd"])
+@pytest.mark.parametrize("B", [4, 20])
+def test_one_sequence_shares_nothing_under_a_tight_bound(B, layout):
+    """max_shared close to max_len: rows of their own are read by one workgroup per pair, the whole of a sequence among them."""
+    lens = [2000 + i % 7 for i in range(B)]
+    shared = [1990] * B
+    shared[1] = 0
+    _run(B, 16, 8 if B == 4 else 2, lens, shared, layout=layout, max_shared=1990, max_len=2010)
+
+
+@pytest.mark.parametrize("B, Hq, Hkv", [(3, 8, 2), (6, 16, 4), (20, 32, 2)])
+def test_each_output_is_that_of_dense_attention(B, Hq, Hkv):
+    """Element by element within what each of the two may be off by, where the first rows are the same.  Together they are closer: the dense
+    launch cuts its weights off at two bf16 terms, 2^-17 too small in the mean, the rest is below that, so 2^-16 of the outputs as a root of the mean square;
+    one row of 700 left out would be about 700^-1/2."""
+    import torch
+    import paper_2603_12038_amd as sfi
+
+    n, m = 700, 90
+    c = ref.Cache(B, Hkv, n + m, "head", seed=81)
+    for t in c.store:
+        t[1:, :, :n] = t[:1, :, :n]
+    ctx = c.context(Hq)
+    try:
+        q = torch.randn((B, Hq, 128), generator=torch.Generator().manual_seed(82)).to(torch.bfloat16).cuda()
+        L = [n + 4 * i for i in range(B)]
+        a, b = torch.zeros((B, Hq, 128), device="cuda"), torch.zeros((B, Hq, 128), device="cuda")
+        _step(f"B={B} heads {Hq}/{Hkv} dense and shared")
+        sfi.sfi_dense_attn(ctx.handle, q, c.K, c.V, i32(L), 0, a)
+        sfi.sfi_shared_attn(ctx.handle, q, c.K, c.V, i32(L), i32([n] * B), B - 1, n, 0, b)
+        torch.cuda.synchronize()
+        K, V, qn = to64(c.numpy(0)), to64(c.numpy(1)), to64(bits(q))
+        a, b = (t.cpu().numpy().astype(np.float64) for t in (a, b))
+        for i in range(B):
+            want, p, size = ref.attend(qn[i], K[i, :, :L[i]], V[i, :, :L[i]])
+            bound = ref.out_bound(p, V[i, :, :L[i]], Hq, size, want, False)
+            assert (np.abs(a[i] - want) <= bound).all() and (np.abs(b[i] - want) <= bound).all() and (np.abs(a[i] - b[i]) <= 2 * bound).all(), i
+        assert np.sqrt(((a - b) ** 2).mean() / (a ** 2).mean()) <= 2.0 ** -16
     finally:
         ctx.close()
