@@ -376,7 +376,8 @@ int sfi_advance(sfi_ctx* ctx, int32_t* ctx_len, int32_t* recent_start, void* str
  *                    more than `high` times in the context the model was trained on are left, below `low` times interpolated
  *   SFI_ROPE_DIMS    the same with s = 1 - clip((i - lo) / (hi - lo), 0, 1), a ramp along the pairs' numbers: lo = floor(i(high)) >= 0,
  *                    hi = ceil(i(low)) <= rot_dim - 1, i(n) = rot_dim ln(orig_ctx / (2 pi n)) / (2 ln base) (hi - lo at least 0.001)
- * rot_dim: a multiple of 16 up to 128.  The angle is exact to 1e-15 of a turn times the position: positions in the millions lose nothing.
+ * rot_dim: a multiple of 16 up to 128.  The angle is exact to 1e-15 of a turn times the position: positions in the millions lose nothing.  Its fraction
+ * of a turn is then rounded to 24 bits, sine, cosine and products are in fp32, and the result is rounded to bf16 once.
  */
 enum { SFI_ROPE_PLAIN = 0, SFI_ROPE_LINEAR = 1, SFI_ROPE_TURNS = 2, SFI_ROPE_DIMS = 3 };
 typedef struct sfi_rope {
@@ -425,8 +426,10 @@ int sfi_rope_append(sfi_ctx* ctx, const void* q, int64_t q_stride_b, int64_t q_s
  *   max_shared  host-side upper bound of shared_len[], in [0, max_len]; it sizes the launch.
  * max_len as in sfi_slow_step, but only rows that are used are read.  Same result as sfi_dense_attn up to the order of the sums and, with a bf16 output and
  * more than 16 queries of a KV head in the batch (B * G), the softmax weights of the shared rows to 2^-17 of themselves.  Rows that only other
- * sequences share may hold anything.  Rows of their own are shared out to the compute units where the batch has few (sequence, KV head) pairs; where it
- * has many, each is read by one workgroup, and a sequence with far more of them than the others has better a call of its own.  Row strides below 2^29.
+ * sequences share may hold anything.  Rows of their own are shared out to the compute units where the batch has few (sequence, KV head) pairs (16 sequences of 8 KV heads on
+ * 256 units) and max_len - max_shared is above 352.  Otherwise one workgroup reads a pair's, however many they are: a sequence that shares far less than max_shared,
+ * or has far more rows of its own than the others, makes the call as long as its own reading takes, and has better a call of its own or, with few pairs, a larger max_len.
+ * Row strides below 2^29.
  */
 int sfi_shared_attn(sfi_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* ctx_len, const int32_t* shared_len,
                     int32_t lead, int32_t max_shared, int32_t max_len, void* out, void* stream);

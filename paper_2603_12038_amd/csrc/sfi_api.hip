@@ -1437,10 +1437,12 @@ void all_rows_view(const sfi_ctx* x, sfi_ctx* y) {
   y->alpha = 1.0f;
 }
 // Splits of the shared rows (none where nothing can be shared): one workgroup per unit.  The sequences' own rows: one workgroup per pair, which needs no
-// records of its own, or, with few pairs and more than three tiles to a wave, all tiles shared out to three workgroups per unit (as many as fit).
-// us, per pair / shared out: 48 pairs, 200, 400, 700, 1200 rows each 8.7 / 11.0, 12.0 / 11.0, 16.0 / 13.6, 22 / 14.4; 128 pairs 10.7 / 12.1, 14.5 / 15.1,
-// 18.8 / 19.7, 26.1 / 25.1, and 24.8 / 19.5 with 100 to 1201 rows; 192 pairs, 700 and 1200 rows 18.8 / 22.2, 27.2 / 30.2; 256 pairs 21 / 26.6, 29.6 / 38, 100 to
-// 1201 rows 28.4 / 28.2.  (Shared out to four to eight per unit: 32 to 33 us where three take 27.)
+// records of its own, or, with few pairs and more than three tiles to a wave, all tiles shared out to three workgroups per unit (as many as fit).  The host
+// knows bounds only: max_len - max_shared stands for the longest sequence's own rows, which one that shares less than max_shared exceeds.
+// us, per pair / shared out, 8 KV heads, rows from memory, flat (paged within 0.8): 48 pairs, 200, 400, 700, 1200 rows each 9.2 / 10.7, 11.9 / 11.1, 14.9 / 14.0, 20.7 / 15.0; 128 pairs
+// 10.3 / 12.1, 13.4 / 15.2, 18.0 / 19.3, 25.1 / 25.5, and 21.8 / 19.1 with 100 to 1201 rows; 192 pairs, 700 and 1200 rows 21.6 / 25.5, 28.9 / 32.6; 256 pairs 25.6 / 29.4, 34.5 / 39.6,
+// 100 to 1201 rows 27.7 / 28.3.  The whole call where one sequence shares nothing and the others 16384 rows (alike: all of them): 4 sequences per pair 174 (21), shared out 36 (23);
+// 32 sequences per pair 183 (31).
 void shared_splits(const sfi_ctx* x, SharedArgs* a) {
   const int cols = shared_cols(a->B * a->G), groups = (a->B * a->G + cols - 1) / cols;
   const int tiles = (a->max_shared + kTile - 1) / kTile;

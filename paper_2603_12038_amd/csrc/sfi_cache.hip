@@ -7,7 +7,8 @@ namespace sfi {
 // ---- rotary positions and append ------------------------------------------------------------------------------
 // Pair i of a head is turned by the angle pos * f_i.  The table holds f_i / 2 pi as a fraction of 2^64 of a turn, so
 // pos * entry mod 2^64 is the angle mod one turn, exact in integers up to the entry's own rounding (pos * 2^-53 turns: 1e-10 at a
-// million), where the product in fp32 would be off by pos * 2^-24 radians.
+// million), where the product in fp32 would be off by pos * 2^-24 radians.  The fraction of a turn goes on as 24 bits of fp32 (2^-25 of half a turn, 1e-7 radians at
+// most), and sine, cosine and products are in fp32: 2^-21 of the terms, hidden behind the one rounding to bf16 (up to 2^-8).
 //
 // A wave has one new row at a time (a token): lane i computes the sine and cosine of pair i once, through LDS they go to the lanes
 // that need them, and the row's heads (query, key, value) follow four at a time, 16 lanes of 16 bytes to a head.
@@ -338,6 +339,8 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
 }
 // Rows are read past the caches (nobody reads them again: 38 -> 32 us for 4 caches of 60000 rows cut to 4261), and written past them where
 // the new caches would not stay there for the next step anyway: 16 x 4092 rows (268 MB) 113 -> 107 us, the 4 x 4261 (70 MB) 32 -> 36.
+// In place: 16 x 5800..6200 rows of 8 KV heads cut to 4092 557 us (into another cache 107), 4 x 30011..60000 cut to 4261, paged, 176 (31), one of 4096 rows of 2 KV heads cut to 1028 5.6
+// (4.0).  What bounds it has not been measured; unlike the copy it stores and reads a flag per workgroup, with release and acquire for the device.
 hipError_t launch_move_rows(const MoveArgs& a, bool in_place, hipStream_t s) {
   const dim3 grid((unsigned)(a.n_chunks + 1) * (unsigned)(a.B * a.Hkv)), block(kMoveThreads);
   const int64_t bytes = (int64_t)a.B * a.Hkv * a.n_chunks * kMoveRows * (4 * kHeadDim);

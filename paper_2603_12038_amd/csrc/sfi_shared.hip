@@ -89,7 +89,7 @@ __device__ __forceinline__ uint4 load16(const char* p) {
 
 // A tile in registers.  A K row leaves as requests of 64 bytes, so the other half of a cache line comes from the L2 if it is left there: K through the caches, V (whole
 // lines at once) past them.  Own rows of 100 to 1201 and 300 rows 23.0 / 20.9 us (K past them too 27.4 / 23.0, V through them too 22.2 / 21.0), 1200 rows each
-// 29.7 (29.8, 36); 16 columns over 32768 / 65536 rows 23.5 / 44.9 (25.2 / 44.8, 23.4 / 50): rows that a case before has left in the last-level cache.
+// 29.7 (29.8, 36); 16 columns over 32768 / 65536 rows 23.5 / 44.9 (25.2 / 44.8, 23.4 / 50).  (Two caches in turn: the last-level cache has part of the rows.)
 struct Tile {
   uint4 ka[4], kb[4], v[8];
 };
@@ -583,8 +583,8 @@ constexpr int kOwnThreads = 64 * kOwnWaves;
 constexpr int kOwnAhead = 8;  // records a thread requests together
 constexpr int kDeviceScope = 16;  // cache-policy bit sc1 of the buffer instructions
 
-// Sequences that differ are evened out here rather than split alike (100 to 1201 rows: 32 us split alike, 30 shared out), and one that shares nothing among
-// others that share 16384 rows is read by as many workgroups as it has records left.
+// Where own rows are shared out (shared_splits), sequences that differ are evened out: 16 sequences of 100 to 1201 rows, 8 KV heads, 19.1 us, one workgroup per pair 21.8; and
+// one that shares nothing among others that share 16384 rows is read by as many workgroups as it has records left.
 // Which part of whose own rows workgroup `slot` of a KV head has, of own_wgs: tiles shared out evenly over the batch, as few to a workgroup as
 // the workgroups allow (at least one for each wave), every sequence at least one workgroup and at most as many as it has records.
 struct OwnShare {
@@ -644,7 +644,8 @@ __device__ __forceinline__ OwnShare own_share(const SharedArgs& a, int slot, int
 }
 
 // A sequence's own rows, one (ALONE) or several workgroups per KV head and sequence, and the merge.  Bound by the rows and the records: 32 sequences of
-// 8 KV heads with 1201 rows each 157 MB in 30 us, 5.3 TB/s; 100 to 1201 rows, paged, 85 MB and 9 MB of the shared rows' records, 28; one row each 8.
+// 8 KV heads with 1200 rows each, 157 MB from memory, in 34.5 us, 4.6 TB/s; 100 to 1201 rows, paged, 85 MB and 9 MB of the shared rows' records, 27.9, and 23.5 where
+// the last-level cache has part of the rows (two such caches in turn); one row each 6.5.
 // A tile per wave on its way: with two, two workgroups fit a unit in place of three, 40 -> 48 us.  The last of a pair's workgroups to finish merges the
 // records of all and those of the shared rows, which the launch before has left, into the output; records go from workgroup to workgroup at
 // device scope (stores and loads that name it, a count once the stores have been performed; the counter is zero between launches).
